@@ -232,6 +232,100 @@ int gear_export_lowrank(const gear_cache* cache, int which, int seg, void* A_f16
 int gear_export_sparse_coo(const gear_cache* cache, int which, int64_t* nnz, void* lin_index_i64,
                            void* value_f16, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * ---- Paged cache --------------------------------------------------------------------------------
+ * K and V of one layer in fixed-size pages that sequences take as they grow: rows are written (and
+ * quantized) as they arrive, one token at a time or a whole prompt, and attention reads them through a
+ * page table.  It is the cache a prompt is prefilled with, chunk by chunk, before gear_compress takes
+ * its rows, the one a decompressed session continues in, and, with codes of 8 or 4 bits, the per-token
+ * grouping (one group = g channels of one token, for Keys and Values alike) that needs no buffer.
+ *
+ * Pool layout (public: a page can be copied, shared or sent as bytes).  Page p starts at p * page_bytes;
+ * inside it KV head h's Keys at 2 h * block_bytes and Values at (2 h + 1) * block_bytes.  A block holds
+ * page_size rows of 16 bits (a row's 128 values as they are), or of b-bit codes (16 b bytes per row):
+ *   8 bits: byte c of the row is channel c's code;
+ *   4 bits: channel 8 w + e is word w's bits 4 (e / 2) + 16 (e % 2) and the three above;
+ * and behind the code rows (scale, zero) words u32 [128 / group][page_size], scale in the low half, both
+ * of the cache's type.  A code stands for the value  scale * code + zero  rounded to the cache's type, with
+ *   zero = min x,  scale = (max x - min x) / (2^b - 1) rounded to the cache's type (the quotient in fp32),
+ *   code = the integer nearest to (x - zero) / scale, halves to even, at most 2^b - 1; 0 where scale is 0
+ * over the group's entries x (Eq. 2).  Slot i is row i % page_size of page i / page_size.
+ */
+typedef enum gear_dtype { GEAR_F16 = 0, GEAR_BF16 = 1 } gear_dtype;
+
+typedef struct gear_page_config {
+  int32_t n_pages;    /* pages of the pool, >= 1                                            */
+  int32_t page_size;  /* tokens per page: 16, 32, 64, 128 or 256                            */
+  int32_t H_kv;       /* KV heads, 1..1024                                                  */
+  int32_t d_h;        /* head dimension, must be 128                                        */
+  int32_t bits;       /* 16 (stored as they are), 8 or 4                                    */
+  int32_t group;      /* g in {32, 64, 128} channels per (scale, zero); not used at 16 bits */
+  int32_t dtype;      /* gear_dtype of rows, queries and outputs                            */
+} gear_page_config;
+
+/* 16-bit values [n_seqs][tokens][heads][128], the 128 contiguous; strides in elements. */
+typedef struct gear_page_rows {
+  void*   data;       /* device, 16-byte aligned; strides multiples of 8 */
+  int64_t seq;
+  int64_t token;
+  int64_t head;
+} gear_page_rows;
+
+/* Which tokens a call of gear_page_attn is about.  The lengths are read on the device, so a captured
+ * call follows them; the int fields bound them and size the launch. */
+typedef struct gear_page_batch {
+  int32_t n_seqs;
+  int32_t n_tokens;             /* rows of q and out (those outside every sequence are not touched)   */
+  int32_t max_q;                /* no sequence has more new tokens; rows beyond that are not computed */
+  int32_t max_kv;               /* about the longest sequence: what the work is divided by            */
+  int32_t table_width;          /* entries of a sequence's row of page_table                          */
+  int32_t causal;               /* 0: every row sees all kv_len tokens                                */
+  const int32_t* q_start;       /* device [n_seqs + 1], ascending: sequence s has rows q_start[s] ..   */
+  const int32_t* kv_len;        /* device [n_seqs]: tokens in the cache, the new ones included         */
+  const int32_t* page_table;    /* device [n_seqs][table_width]: tokens page_size i .. are in page [i] */
+} gear_page_batch;
+
+/* Bytes of a pool.  GEAR_ECAPACITY if a page has 2 GiB or more. */
+int gear_page_bytes(const gear_page_config* cfg, size_t* pool_bytes);
+
+/*
+ * Writes row (s, t, h) of K and V into slot slots[s * n_rows + t] of head h, for all s < n_seqs, t < n_rows.
+ * slots     : device int64.  A slot outside 0 .. n_pages * page_size - 1 (-1: padding) is skipped.  A slot
+ *             should be named once: of one that is named twice the bytes may come from either row.
+ * Values must be finite, and below 2^126 in magnitude where they are quantized.
+ */
+int gear_page_write(const gear_page_config* cfg, void* pool, size_t pool_bytes, const gear_page_rows* K,
+                    const gear_page_rows* V, int32_t n_seqs, int32_t n_rows, const int64_t* slots, void* stream);
+
+/* The reverse: the values that slot slots[s * n_rows + t] stands for into row (s, t, h) of K and V (either may
+ * be NULL).  Rows whose slot is outside the pool are left as they are.  With seq, token and head strides
+ * of a [B, H_kv, n, 128] tensor the rows come as gear_compress takes them. */
+int gear_page_read(const gear_page_config* cfg, const void* pool, size_t pool_bytes, const gear_page_rows* K,
+                   const gear_page_rows* V, int32_t n_seqs, int32_t n_rows, const int64_t* slots, void* stream);
+
+/* Workspace of gear_page_attn for H_q query heads and every batch with at most these n_seqs, n_tokens, max_q and
+ * max_kv (0 where no axis is divided).  Only the int fields of `batch` are read. */
+int gear_page_attn_bytes(const gear_page_config* cfg, int32_t H_q, const gear_page_batch* batch, size_t* workspace_bytes);
+
+/*
+ * Attention of each sequence's new tokens over its pages, which hold them already: with n = q_start[s + 1] -
+ * q_start[s], row i (0-based) of sequence s is its token kv_len[s] - n + i and sees the tokens up to and with
+ * itself (causal) or all kv_len[s]:
+ *     out = softmax(scale * q K^T) V  over the values the pages' rows stand for;
+ * query head j reads KV head j / (H_q / H_kv).  Any mix of single tokens, a few rows and whole chunks.  A row that
+ * sees nothing is 0.  Scores, softmax statistics and sums are held in fp32; the weights are rounded to the
+ * cache's type for the product with V.
+ * q, out    : rows [n_tokens][H_q][128] (seq strides not used), dtype of cfg.
+ * H_q       : a multiple of H_kv.
+ * page_table: entries outside 0 .. n_pages - 1 are not followed: their tokens are not seen.  kv_len is
+ *             taken as table_width * page_size where it is more.
+ * workspace : device, >= the bytes of gear_page_attn_bytes, 16-byte aligned; NULL where those are 0.  Nothing in
+ *             it need survive, but calls that may run at the same time need one each.
+ */
+int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_bytes, const gear_page_batch* batch,
+                   const gear_page_rows* q, int32_t H_q, float scale, const gear_page_rows* out, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
 const char* gear_strerror(int status);
 
 #ifdef __cplusplus

@@ -16,6 +16,7 @@ GEAR_OK, GEAR_EINVAL, GEAR_ECAPACITY, GEAR_EALIGN, GEAR_EHIP = 0, -1, -2, -3, -4
 EXPORTED = [
     "gear_cache_bytes", "gear_cache_init", "gear_cache_reset", "gear_compress", "gear_compress_recent", "gear_decompress",
     "gear_decode_attn", "gear_decode_attn_mq", "gear_decode_attn_static", "gear_export_codes", "gear_export_sparse", "gear_export_sparse_coo", "gear_export_lowrank", "gear_strerror",
+    "gear_page_bytes", "gear_page_write", "gear_page_read", "gear_page_attn_bytes", "gear_page_attn",
 ]
 
 
@@ -37,6 +38,22 @@ class gear_cache(ctypes.Structure):
         ("chunk_n", ctypes.c_uint8 * GEAR_MAX_CHUNKS),
         ("chunk_rank", ctypes.c_uint8 * GEAR_MAX_CHUNKS),
     ]
+
+
+class gear_page_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "H_kv", "d_h", "bits", "group", "dtype")]
+
+
+class gear_page_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("seq", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class gear_page_batch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "n_tokens", "max_q", "max_kv", "table_width", "causal")] + \
+               [(n, ctypes.c_void_p) for n in ("q_start", "kv_len", "page_table")]
+
+
+GEAR_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
 
 
 class GearError(RuntimeError):
@@ -71,6 +88,12 @@ def load_library():
     lib.gear_export_sparse.argtypes = [cachep, ctypes.c_int, vp, vp, vp]
     lib.gear_export_sparse_coo.argtypes = [cachep, ctypes.c_int, ctypes.POINTER(ctypes.c_int64), vp, vp, vp, sz, vp]
     lib.gear_export_lowrank.argtypes = [cachep, ctypes.c_int, ctypes.c_int, vp, vp, vp]
+    pcfg, rows, batch = (ctypes.POINTER(t) for t in (gear_page_config, gear_page_rows, gear_page_batch))
+    lib.gear_page_bytes.argtypes = [pcfg, ctypes.POINTER(sz)]
+    lib.gear_page_write.argtypes = [pcfg, vp, sz, rows, rows, i32, i32, vp, vp]
+    lib.gear_page_read.argtypes = [pcfg, vp, sz, rows, rows, i32, i32, vp, vp]
+    lib.gear_page_attn_bytes.argtypes = [pcfg, i32, batch, ctypes.POINTER(sz)]
+    lib.gear_page_attn.argtypes = [pcfg, vp, sz, batch, rows, i32, ctypes.c_float, rows, vp, sz, vp]
     lib.gear_strerror.argtypes = [ctypes.c_int]
     lib.gear_strerror.restype = ctypes.c_char_p
     for name in EXPORTED:
@@ -198,6 +221,99 @@ def gear_export_lowrank(cache, which, seg, A, Bf):
            "gear_export_lowrank")
 
 
+# ---- the paged cache: rows are tensors [n_seqs, tokens, heads, 128] (or [tokens, heads, 128]) of the pool's type, of any
+# strides that the C ABI takes; a view of [n_seqs, heads, tokens, 128] is x.transpose(1, 2).  What is about to be read as
+# something that it is not (another type, device or shape) is refused here, with ValueError, since the library sees pointers only.
+def make_page_config(n_pages, page_size, H_kv, bits, group=128, dtype=torch.float16, d_h=128):
+    return gear_page_config(n_pages, page_size, H_kv, d_h, bits, group, GEAR_DTYPES[dtype])
+
+
+def _here(t, what):
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError("%s lies on %s, not on the current GPU" % (what, t.device))
+
+
+def _page_rows(t, cfg, heads, what):
+    """(the view, sequences, tokens) of a tensor of rows."""
+    if t.dim() not in (3, 4) or t.shape[-1] != cfg.d_h or t.shape[-2] != heads:
+        raise ValueError("%s is [n_seqs, tokens, %d, %d] or without the first: got %s" % (what, heads, cfg.d_h, tuple(t.shape)))
+    if GEAR_DTYPES.get(t.dtype) != cfg.dtype or t.stride(-1) != 1:
+        raise ValueError("%s: another type than the pool's, or a row that is not contiguous" % what)
+    _here(t, what)
+    s = t.stride()
+    if t.dim() == 3:
+        return gear_page_rows(t.data_ptr(), 0, s[0], s[1]), 1, t.shape[0]
+    return gear_page_rows(t.data_ptr(), s[0], s[1], s[2]), t.shape[0], t.shape[1]
+
+
+def _page_index(t, dtype, n, what):
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s is a contiguous %s tensor of %d entries: got %s %s" % (what, dtype, n, t.dtype, tuple(t.shape)))
+    _here(t, what)
+    return t.data_ptr()
+
+
+def _page_pool(pool):
+    if not pool.is_contiguous():
+        raise ValueError("the pool is one contiguous tensor")
+    _here(pool, "the pool")
+    return pool.data_ptr(), _bytes(pool)
+
+
+def gear_page_bytes(cfg):
+    n = ctypes.c_size_t(0)
+    _check(load_library().gear_page_bytes(ctypes.byref(cfg), ctypes.byref(n)), "gear_page_bytes")
+    return n.value
+
+
+def _page_copy(name, cfg, pool, K, V, slots):
+    k, v = (None if t is None else _page_rows(t, cfg, cfg.H_kv, w) for t, w in ((K, "K"), (V, "V")))
+    some = k or v
+    if some is None:
+        raise ValueError("neither K nor V is given")
+    if k and v and k[1:] != v[1:]:
+        raise ValueError("K and V differ in their rows: %s and %s" % (tuple(K.shape), tuple(V.shape)))
+    p, n = _page_pool(pool)
+    at = _page_index(slots, torch.int64, some[1] * some[2], "slots")
+    _check(getattr(load_library(), name)(ctypes.byref(cfg), p, n, k and ctypes.byref(k[0]), v and ctypes.byref(v[0]), some[1], some[2], at,
+                                         _stream()), name)
+
+
+def gear_page_write(cfg, pool, K, V, slots):
+    _page_copy("gear_page_write", cfg, pool, K, V, slots)
+
+
+def gear_page_read(cfg, pool, K_out, V_out, slots):
+    _page_copy("gear_page_read", cfg, pool, K_out, V_out, slots)
+
+
+def make_page_batch(q_start, kv_len, page_table, n_tokens, max_q, max_kv, causal=True):
+    """The batch of a gear_page_attn call (one serves all layers of a step): int32 tensors q_start [n_seqs + 1], kv_len [n_seqs],
+    page_table [n_seqs, width].  It keeps them alive."""
+    n, width = page_table.shape
+    b = gear_page_batch(n, n_tokens, max_q, max_kv, width, 1 if causal else 0, _page_index(q_start, torch.int32, n + 1, "q_start"),
+                        _page_index(kv_len, torch.int32, n, "kv_len"), _page_index(page_table, torch.int32, n * width, "page_table"))
+    b.tensors = (q_start, kv_len, page_table)
+    return b
+
+
+def gear_page_attn_bytes(cfg, H_q, batch):
+    n = ctypes.c_size_t(0)
+    _check(load_library().gear_page_attn_bytes(ctypes.byref(cfg), H_q, ctypes.byref(batch), ctypes.byref(n)), "gear_page_attn_bytes")
+    return n.value
+
+
+def gear_page_attn(cfg, pool, batch, q, out, scale, workspace):
+    H_q = q.shape[-2]
+    a, b = _page_rows(q, cfg, H_q, "q"), _page_rows(out, cfg, H_q, "out")
+    if q.dim() != 3 or out.dim() != 3 or a[2] != batch.n_tokens or b[2] != batch.n_tokens:
+        raise ValueError("q and out are [%d, H_q, %d]: got %s and %s" % (batch.n_tokens, cfg.d_h, tuple(q.shape), tuple(out.shape)))
+    p, n = _page_pool(pool)
+    w, wn = (None, 0) if workspace is None else _page_pool(workspace)
+    _check(load_library().gear_page_attn(ctypes.byref(cfg), p, n, ctypes.byref(batch), ctypes.byref(a[0]), H_q, scale, ctypes.byref(b[0]), w,
+                                         wn, _stream()), "gear_page_attn")
+
+
 # ---- convenience owner of the device buffers -------------------------------
 class GearCache:
     """Allocates the arena and workspace with torch and forwards to the C ABI."""
@@ -289,3 +405,38 @@ class GearCache:
         if r > 0:
             gear_export_lowrank(self.cache, which, seg, A, Bf)
         return A, Bf
+
+
+class PagePool:
+    """Allocates a pool of pages, and the workspace of its reads as they need it; forwards to the C ABI."""
+
+    def __init__(self, cfg, device="cuda:0"):
+        self.cfg = cfg
+        self.device = torch.device(device)
+        self.pool = torch.zeros(gear_page_bytes(cfg), dtype=torch.uint8, device=self.device)
+
+    def write(self, K, V, slots):
+        gear_page_write(self.cfg, self.pool, K, V, slots)
+
+    def read(self, slots, heads_first=False):
+        """K, V of slots [n_seqs, tokens] as [n_seqs, tokens, H_kv, 128], or [n_seqs, H_kv, tokens, 128]: what GearCache.compress takes.
+        Rows whose slot is outside the pool are 0."""
+        c, (n, m) = self.cfg, slots.shape
+        dt = {v: k for k, v in GEAR_DTYPES.items()}[c.dtype]
+        shape = (n, c.H_kv, m, c.d_h) if heads_first else (n, m, c.H_kv, c.d_h)
+        K, V = (torch.zeros(shape, dtype=dt, device=self.device) for _ in range(2))
+        gear_page_read(c, self.pool, K.transpose(1, 2) if heads_first else K, V.transpose(1, 2) if heads_first else V, slots)
+        return K, V
+
+    def workspace_for(self, H_q, batch):
+        """A workspace for this batch and all smaller ones (None where none is needed)."""
+        n = gear_page_attn_bytes(self.cfg, H_q, batch)
+        return torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+
+    def attn(self, q, batch, scale=None, out=None, workspace=None):
+        if out is None:
+            out = torch.empty_like(q)
+        if workspace is None:
+            workspace = self.workspace_for(q.shape[-2], batch)
+        gear_page_attn(self.cfg, self.pool, batch, q, out, self.cfg.d_h ** -0.5 if scale is None else scale, workspace)
+        return out

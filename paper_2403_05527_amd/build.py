@@ -11,13 +11,17 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libgear.so")
 
-SOURCES = ["gear_api.hip", "compress_filter.hip", "compress_values.hip", "lowrank.hip", "decode.hip", "decompress_export.hip"]
+CSRC_PAGES = os.path.join(PKG, "csrc_pages")   # the paged cache
+
+SOURCES = [os.path.join(CSRC, s) for s in ("gear_api.hip", "compress_filter.hip", "compress_values.hip", "lowrank.hip", "decode.hip",
+                                           "decompress_export.hip")]
+SOURCES += [os.path.join(CSRC_PAGES, s) for s in ("page_api.hip", "page_copy.hip", "page_few.hip", "page_many.hip")]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wno-unused-command-line-argument", "-Wno-unknown-warning-option",
-    "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+    "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-I", CSRC_PAGES,
 ]
 
 
@@ -42,8 +46,8 @@ def kernel_resources(stderr_text):
 
 
 def _compile(src):
-    obj = os.path.join(OBJ, src.replace(".hip", ".o"))
-    cmd = ["hipcc", "-c", os.path.join(CSRC, src), "-o", obj, "-Rpass-analysis=kernel-resource-usage"] + FLAGS
+    obj = os.path.join(OBJ, os.path.basename(src).replace(".hip", ".o"))
+    cmd = ["hipcc", "-c", src, "-o", obj, "-Rpass-analysis=kernel-resource-usage"] + FLAGS
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("hipcc failed for %s:\n%s\n%s" % (src, r.stdout, r.stderr))

@@ -1,0 +1,228 @@
+// Entry points of the paged cache (include/gear.h): arguments are checked here, before anything is launched.
+#include <cmath>
+#include "page_launch.h"
+
+namespace gear {
+
+// How the key axis is divided.  Blocks of either kernel that the chip holds at once; the axis is divided until there are about
+// as many, in parts of at least FEW_PART / MANY_PART tokens.
+#ifndef GEAR_PAGE_CUS   // (the CPU stand-in sets it, so that its small cases are divided)
+#define GEAR_PAGE_CUS GEAR_CUS
+#endif
+constexpr int FEW_SLOTS = 3 * GEAR_PAGE_CUS, MANY_SLOTS = 2 * GEAR_PAGE_CUS;
+constexpr int FEW_COLS_MOST = 32;
+
+static int split_by(int64_t blocks, int slots, int max_kv, int least) {
+  const int by_keys = max_kv / least, by_slots = blocks > 0 ? (int)(slots / blocks) : 1;
+  const int n = by_keys < by_slots ? by_keys : by_slots;
+  return n < 1 ? 1 : n;
+}
+
+PagePlan page_plan(int H, int gq, int n_seqs, int n_tokens, int max_q, int max_kv) {
+  PagePlan p{};
+  const int64_t cols = (int64_t)max_q * gq;
+  const bool all_few = cols <= FEW_COLS_MOST;
+  // (a batch that is not n_seqs x max_q has shorter sequences, single tokens for instance)
+  p.few = all_few || ((int64_t)n_seqs * max_q != n_tokens && gq <= FEW_COLS_MOST);
+  p.many = !all_few;
+  p.few_limit = p.few ? (all_few ? (int)cols : FEW_COLS_MOST) : 0;
+  p.few_tiles = p.few_limit <= 16 ? 1 : 2;
+  p.few_split = p.many_split = 1;
+  if (p.few) {
+    p.few_split = split_by((int64_t)n_seqs * H, FEW_SLOTS, max_kv, FEW_PART);
+    if (p.few_split > 1) p.few_rows = (int64_t)n_seqs * H * p.few_limit;
+  }
+  if (p.many) {
+    const int64_t tiles = ((int64_t)n_tokens * gq + MANY_COLS - 1) / MANY_COLS;
+    p.many_split = split_by(tiles * H, MANY_SLOTS, max_kv, MANY_PART);
+    if (p.many_split > 1) p.many_rows = (int64_t)n_tokens * H * gq;
+  }
+  return p;
+}
+
+int64_t page_records_most(int H, int gq, int n_seqs, int n_tokens, int max_q, int max_kv) {
+  // rows x parts of either kernel, each bounded by what the slots allow and by what the keys allow
+  const int64_t few_cols = (int64_t)max_q * gq < FEW_COLS_MOST ? (int64_t)max_q * gq : FEW_COLS_MOST;
+  int64_t few = 0, many = 0;
+  if (max_kv / FEW_PART > 1) {
+    const int64_t by_keys = (int64_t)n_seqs * H * (max_kv / FEW_PART), blocks = by_keys < FEW_SLOTS ? by_keys : FEW_SLOTS;
+    few = blocks * few_cols;
+  }
+  if ((int64_t)max_q * gq > FEW_COLS_MOST && max_kv / MANY_PART > 1) {
+    const int64_t by_keys = (int64_t)n_tokens * H * gq * (max_kv / MANY_PART), by_slots = (int64_t)MANY_SLOTS * MANY_COLS;
+    many = by_keys < by_slots ? by_keys : by_slots;
+  }
+  return few + many;
+}
+
+}  // namespace gear
+
+using namespace gear;
+
+namespace {
+
+constexpr size_t RECORD_BYTES = (2 + D) * sizeof(float);
+constexpr int64_t INT_MOST = 0x7FFFFFFF;
+
+int check_page_config(const gear_page_config* c, size_t* pool_bytes, PageGeom* g) {
+  if (!c) return GEAR_EINVAL;
+  if (c->d_h != D || c->n_pages < 1 || c->H_kv < 1 || c->H_kv > 1024) return GEAR_EINVAL;
+  if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1))) return GEAR_EINVAL;
+  if (c->bits != 16 && c->bits != 8 && c->bits != 4) return GEAR_EINVAL;
+  if (c->bits != 16 && c->group != 32 && c->group != 64 && c->group != 128) return GEAR_EINVAL;
+  if (c->dtype != GEAR_F16 && c->dtype != GEAR_BF16) return GEAR_EINVAL;
+  const int group = c->bits == 16 ? D : c->group;
+  g->row_bytes = (uint32_t)(D * c->bits / 8);
+  g->block_bytes = (uint32_t)c->page_size * (g->row_bytes + (c->bits == 16 ? 0u : 4u * (uint32_t)(D / group)));
+  g->page_bytes = 2ull * (uint64_t)c->H_kv * g->block_bytes;
+  g->n_pages = c->n_pages;
+  g->shift = __builtin_ctz((unsigned)c->page_size);
+  g->gshift = __builtin_ctz((unsigned)group);
+  g->H = c->H_kv;
+  g->pool = nullptr;
+  if (g->page_bytes >= (1ull << 31)) return GEAR_ECAPACITY;
+  *pool_bytes = (size_t)g->page_bytes * (size_t)c->n_pages;
+  return GEAR_OK;
+}
+
+bool misaligned(const void* p, uintptr_t by) { return (reinterpret_cast<uintptr_t>(p) & (by - 1)) != 0; }
+
+int check_pool(const gear_page_config* cfg, const void* pool, size_t pool_bytes, PageGeom* g) {
+  size_t need = 0;
+  const int rc = check_page_config(cfg, &need, g);
+  if (rc) return rc;
+  if (!pool) return GEAR_EINVAL;
+  if (misaligned(pool, 16)) return GEAR_EALIGN;
+  if (pool_bytes < need) return GEAR_ECAPACITY;
+  g->pool = static_cast<const unsigned char*>(pool);
+  return GEAR_OK;
+}
+
+// written: two rows must not share their place (where there are two)
+int check_rows(const gear_page_rows* r, int64_t n_seqs, int64_t n_rows, int64_t heads, bool written) {
+  if (!r->data) return GEAR_EINVAL;
+  if (misaligned(r->data, 16) || (n_seqs > 1 && r->seq % 8) || (n_rows > 1 && r->token % 8) || (heads > 1 && r->head % 8)) return GEAR_EALIGN;
+  if (written && ((n_seqs > 1 && r->seq == 0) || (n_rows > 1 && r->token == 0) || (heads > 1 && r->head == 0))) return GEAR_EINVAL;
+  return GEAR_OK;
+}
+RowView view_of(const gear_page_rows* r) {
+  return r ? RowView{static_cast<unsigned char*>(r->data), r->seq, r->token, r->head} : RowView{nullptr, 0, 0, 0};
+}
+
+int copy_rows(const gear_page_config* cfg, const void* pool, size_t pool_bytes, const gear_page_rows* K, const gear_page_rows* V,
+              int32_t n_seqs, int32_t n_rows, const int64_t* slots, bool write, void* stream) {
+  PageGeom g;
+  int rc = check_pool(cfg, pool, pool_bytes, &g);
+  if (rc) return rc;
+  if (n_seqs < 0 || n_rows < 0 || (write ? !K || !V : !K && !V)) return GEAR_EINVAL;
+  const int64_t total = (int64_t)n_seqs * n_rows;
+  if (K && (rc = check_rows(K, n_seqs, n_rows, cfg->H_kv, !write))) return rc;
+  if (V && (rc = check_rows(V, n_seqs, n_rows, cfg->H_kv, !write))) return rc;
+  if (total == 0) return GEAR_OK;
+  if (!slots) return GEAR_EINVAL;
+  if (misaligned(slots, 8)) return GEAR_EALIGN;
+  if (total > INT_MOST - 4096 || (total + 15) / 16 * cfg->H_kv > INT_MOST) return GEAR_ECAPACITY;
+  return launch_page_copy(g, cfg->bits, cfg->dtype == GEAR_BF16, write, view_of(K), view_of(V), slots, n_seqs, n_rows,
+                          static_cast<hipStream_t>(stream)) == hipSuccess ? GEAR_OK : GEAR_EHIP;
+}
+
+int check_batch(const gear_page_config* cfg, int32_t H_q, const gear_page_batch* b) {
+  if (!b || H_q < 1 || H_q % cfg->H_kv) return GEAR_EINVAL;
+  if (b->n_seqs < 0 || b->n_tokens < 0 || b->max_q < 0 || b->max_kv < 0) return GEAR_EINVAL;
+  // (all indices of columns, blocks and records' rows are 32-bit numbers)
+  if ((int64_t)b->n_tokens * H_q > INT_MOST || (int64_t)b->max_q * H_q > INT_MOST) return GEAR_ECAPACITY;
+  if ((int64_t)b->n_seqs * H_q * FEW_COLS_MOST > INT_MOST) return GEAR_ECAPACITY;
+  return GEAR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int gear_page_bytes(const gear_page_config* cfg, size_t* pool_bytes) {
+  PageGeom g;
+  size_t need = 0;
+  const int rc = check_page_config(cfg, &need, &g);
+  if (rc) return rc;
+  if (!pool_bytes) return GEAR_EINVAL;
+  *pool_bytes = need;
+  return GEAR_OK;
+}
+
+int gear_page_write(const gear_page_config* cfg, void* pool, size_t pool_bytes, const gear_page_rows* K, const gear_page_rows* V,
+                    int32_t n_seqs, int32_t n_rows, const int64_t* slots, void* stream) {
+  return copy_rows(cfg, pool, pool_bytes, K, V, n_seqs, n_rows, slots, true, stream);
+}
+
+int gear_page_read(const gear_page_config* cfg, const void* pool, size_t pool_bytes, const gear_page_rows* K, const gear_page_rows* V,
+                   int32_t n_seqs, int32_t n_rows, const int64_t* slots, void* stream) {
+  return copy_rows(cfg, pool, pool_bytes, K, V, n_seqs, n_rows, slots, false, stream);
+}
+
+int gear_page_attn_bytes(const gear_page_config* cfg, int32_t H_q, const gear_page_batch* batch, size_t* workspace_bytes) {
+  PageGeom g;
+  size_t need = 0;
+  int rc = check_page_config(cfg, &need, &g);
+  if (rc || (rc = check_batch(cfg, H_q, batch))) return rc;
+  if (!workspace_bytes) return GEAR_EINVAL;
+  *workspace_bytes = RECORD_BYTES * (size_t)page_records_most(cfg->H_kv, H_q / cfg->H_kv, batch->n_seqs, batch->n_tokens, batch->max_q, batch->max_kv);
+  return GEAR_OK;
+}
+
+int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_bytes, const gear_page_batch* batch, const gear_page_rows* q,
+                   int32_t H_q, float scale, const gear_page_rows* out, void* workspace, size_t workspace_bytes, void* stream) {
+  PageAttn a{};
+  int rc = check_pool(cfg, pool, pool_bytes, &a.geom);
+  if (rc || (rc = check_batch(cfg, H_q, batch))) return rc;
+  const gear_page_batch& b = *batch;
+  if (!q || !out || !std::isfinite(scale)) return GEAR_EINVAL;
+  if ((rc = check_rows(q, 1, b.n_tokens, H_q, false)) || (rc = check_rows(out, 1, b.n_tokens, H_q, true))) return rc;
+  if (b.n_seqs == 0 || b.n_tokens == 0 || b.max_q == 0) return GEAR_OK;
+  if (!b.q_start || !b.kv_len || b.table_width < 0 || (b.table_width > 0 && !b.page_table)) return GEAR_EINVAL;
+  if (misaligned(b.q_start, 4) || misaligned(b.kv_len, 4) || misaligned(b.page_table, 4) || misaligned(workspace, 16)) return GEAR_EALIGN;
+  if ((int64_t)b.table_width * cfg->page_size > INT_MOST - 1024) return GEAR_ECAPACITY;
+  const int H = cfg->H_kv, gq = H_q / H;
+  const PagePlan p = page_plan(H, gq, b.n_seqs, b.n_tokens, b.max_q, b.max_kv);
+  const int64_t few_recs = p.few_rows * p.few_split, many_recs = p.many_rows * p.many_split;
+  if (few_recs + many_recs > 0) {
+    if (!workspace) return GEAR_EINVAL;
+    if (workspace_bytes < RECORD_BYTES * (size_t)(few_recs + many_recs)) return GEAR_ECAPACITY;
+  }
+  const int64_t tiles = (int64_t)b.n_tokens * gq / MANY_COLS + b.n_seqs;
+  if ((int64_t)b.n_seqs * H * p.few_split > INT_MOST || tiles * H * p.many_split > INT_MOST) return GEAR_ECAPACITY;
+
+  a.q_start = b.q_start;
+  a.kv_len = b.kv_len;
+  a.table = b.page_table;
+  a.q = view_of(q);
+  a.out = view_of(out);
+  a.scale_log2 = scale * 1.44269504088896340736f;
+  a.width = b.table_width;
+  a.n_seqs = b.n_seqs;
+  a.n_tokens = b.n_tokens;
+  a.gq = gq;
+  a.causal = b.causal ? 1 : 0;
+  a.few = p.few_limit;
+  a.few_cols = p.few_limit;
+  a.tiles = (int32_t)tiles;
+  float* rec = static_cast<float*>(workspace);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const bool bf = cfg->dtype == GEAR_BF16;
+  if (p.many) {   // the longer kernel first
+    PageAttn m = a;
+    m.n_split = p.many_split;
+    m.rec_o = rec;
+    m.rec_ml = reinterpret_cast<float2*>(rec + many_recs * D);
+    if (launch_page_many(m, cfg->bits, bf, st) != hipSuccess) return GEAR_EHIP;
+  }
+  if (p.few) {
+    PageAttn f = a;
+    f.n_split = p.few_split;
+    f.rec_o = rec + many_recs * (D + 2);
+    f.rec_ml = reinterpret_cast<float2*>(f.rec_o + few_recs * D);
+    if (launch_page_few(f, cfg->bits, bf, p.few_tiles, st) != hipSuccess) return GEAR_EHIP;
+  }
+  return GEAR_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,243 @@
+// Shared by the kernels of the paged cache: the pool's geometry, conversions between codes and values, and the
+// matrix instructions in both 16-bit types.
+#pragma once
+#include "gear_internal.h"
+
+// v_mfma with 16-bit operands and fp32 accumulators (a build that runs the kernels elsewhere may predefine these).
+// 16x16x32: A lane l = row l % 16, k = 8 (l / 16) + 0..7; B the same for columns; D lane l = rows 4 (l / 16) + 0..3, column l % 16.
+// 32x32x16: A lane l = row l % 32, k = 8 (l / 32) + 0..7; B the same for columns; D lane l, register i = row 8 (i / 4) + 4 (l / 32)
+// + i % 4, column l % 32.
+#ifndef GEAR_MFMA16_F16
+#define GEAR_MFMA16_F16(a, b, c) \
+  __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(gear::h8_t, (a)), __builtin_bit_cast(gear::h8_t, (b)), (c), 0, 0, 0)
+#define GEAR_MFMA16_BF16(a, b, c) \
+  __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(gear::b8_t, (a)), __builtin_bit_cast(gear::b8_t, (b)), (c), 0, 0, 0)
+#define GEAR_MFMA32_F16(a, b, c) \
+  __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(gear::h8_t, (a)), __builtin_bit_cast(gear::h8_t, (b)), (c), 0, 0, 0)
+#define GEAR_MFMA32_BF16(a, b, c) \
+  __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(gear::b8_t, (a)), __builtin_bit_cast(gear::b8_t, (b)), (c), 0, 0, 0)
+#endif
+// ds_read_b64_tr_b16: in each group of 16 lanes, lane i addresses 8 bytes, row i / 4 and columns 4 (i % 4) + 0..3 of a 4 x 16
+// matrix of 16-bit values, and gets column i's four rows.
+#ifndef GEAR_LDS_READ_TR
+#define GEAR_LDS_READ_TR(p) \
+  __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) gear::s4_t*)(p)))
+#endif
+#ifndef GEAR_EXP2
+#define GEAR_EXP2(x) __builtin_amdgcn_exp2f(x)
+#endif
+// two floats as bf16 values (nearest even), the first in the low half: one instruction
+#ifndef GEAR_PACK_BF2
+#define GEAR_PACK_BF2(a, b) __builtin_bit_cast(uint32_t, (gear::b2_t){(__bf16)(a), (__bf16)(b)})
+#endif
+// a * b + c on two pairs of fp16 values, each rounded once
+#ifndef GEAR_PK_FMA_F16
+#define GEAR_PK_FMA_F16(a, b, c)                                                                                            \
+  __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(gear::h2_t, (a)), __builtin_bit_cast(gear::h2_t, (b)), \
+                                                         __builtin_bit_cast(gear::h2_t, (c))))
+#endif
+
+namespace gear {
+
+typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
+#ifndef GEAR_NO_BF16_TYPE
+typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 b2_t __attribute__((ext_vector_type(2)));
+#endif
+typedef short s4_t __attribute__((ext_vector_type(4)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+
+// The pool as the kernels see it.
+struct PageGeom {
+  const unsigned char* pool;
+  uint64_t page_bytes;
+  uint32_t block_bytes;   // Keys or Values of one head in a page
+  uint32_t row_bytes;
+  int32_t n_pages;
+  int32_t shift;          // log2 of the page size
+  int32_t gshift;         // log2 of the group size
+  int32_t H;
+};
+__host__ __device__ inline uint32_t page_mask(const PageGeom& g) { return (1u << g.shift) - 1u; }
+__host__ __device__ inline uint32_t words_at(const PageGeom& g) { return g.row_bytes << g.shift; }   // the (scale, zero) words in a block
+
+// 16-bit rows with strides in elements
+struct RowView {
+  unsigned char* data;
+  int64_t seq, token, head;
+};
+
+// ---- 16-bit values ----------------------------------------------------------
+template <bool BF>
+__device__ __forceinline__ float to_f32(uint32_t bits16) {
+  if constexpr (BF) return __uint_as_float(bits16 << 16);
+  else return h2f(bits16 & 0xFFFFu);
+}
+template <bool BF>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {   // rounded to nearest even, a in the low half
+  if constexpr (BF) return GEAR_PACK_BF2(a, b);
+  else return pack_h2(a, b);
+}
+template <bool BF>
+__device__ __forceinline__ floatx4 mfma16(const uint4& a, const uint4& b, const floatx4& c) {
+  if constexpr (BF) return GEAR_MFMA16_BF16(a, b, c);
+  else return GEAR_MFMA16_F16(a, b, c);
+}
+template <bool BF>
+__device__ __forceinline__ floatx16 mfma32(const uint4& a, const uint4& b, const floatx16& c) {
+  if constexpr (BF) return GEAR_MFMA32_BF16(a, b, c);
+  else return GEAR_MFMA32_F16(a, b, c);
+}
+
+// ---- codes to values ----------------------------------------------------------
+// Two codes as integers in the halves of a word, as the arithmetic of the type wants them: fp16 has them as 1024 + code or 64 + code
+// (the low mantissa bits of those numbers), bf16 goes through fp32.
+// (scale, zero) words of the two entries: `sz0` for the low one.  The same word twice where both lie in one group of a row.
+struct PairScale {
+  uint32_t scale, zero;   // fp16: a pair each
+  float s0, z0, s1, z1;   // bf16
+};
+template <bool BF>
+__device__ __forceinline__ PairScale pair_scale(uint32_t sz0, uint32_t sz1) {
+  PairScale p;
+  if constexpr (BF) {
+    p.s0 = __uint_as_float(sz0 << 16);
+    p.z0 = __uint_as_float(sz0 & 0xFFFF0000u);
+    p.s1 = __uint_as_float(sz1 << 16);
+    p.z1 = __uint_as_float(sz1 & 0xFFFF0000u);
+  } else {
+    p.scale = GEAR_BYTE_PERM(sz1, sz0, 0x05040100u);
+    p.zero = GEAR_BYTE_PERM(sz1, sz0, 0x07060302u);
+  }
+  return p;
+}
+constexpr uint32_t F16_1024 = 0x64006400u, F16_64 = 0x54005400u, F16_NEG_1024 = 0xE400E400u, F16_NEG_64 = 0xD400D400u;
+// fp16: value pair of (1024 + code) or (64 + code) pairs.  Both steps are exact but for the one rounding of the fused multiply-add:
+// the value that a code stands for.
+__device__ __forceinline__ uint32_t value_f16(uint32_t biased, uint32_t neg_bias, const PairScale& p) {
+  const uint32_t c = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2_t, biased) + __builtin_bit_cast(h2_t, neg_bias));
+  return GEAR_PK_FMA_F16(c, p.scale, p.zero);
+}
+__device__ __forceinline__ uint32_t value_bf16(uint32_t c0, uint32_t c1, const PairScale& p) {
+  return GEAR_PACK_BF2(__builtin_fmaf((float)c0, p.s0, p.z0), __builtin_fmaf((float)c1, p.s1, p.z1));
+}
+// Channels 2 i, 2 i + 1 (i = 0..3) of a run of eight along a row: w0, w1 are the run's code words (w1 at 8 bits only).
+template <int BITS, bool BF>
+__device__ __forceinline__ uint32_t row_pair(uint32_t w0, uint32_t w1, int i, const PairScale& p) {
+  if constexpr (BITS == 8) {
+    const uint32_t w = i < 2 ? w0 : w1;
+    if constexpr (BF) {
+      return value_bf16((w >> (16 * (i & 1))) & 0xFFu, (w >> (16 * (i & 1) + 8)) & 0xFFu, p);
+    } else {
+      return value_f16(GEAR_BYTE_PERM(F16_1024 | 0x00640064u, w, (i & 1) ? 0x04030402u : 0x04010400u), F16_NEG_1024, p);
+    }
+  } else {   // 4 bits: nibble i of each half
+    if constexpr (BF) {
+      return value_bf16((w0 >> (4 * i)) & 0xFu, (w0 >> (4 * i + 16)) & 0xFu, p);
+    } else {
+      const uint32_t x = i < 2 ? w0 : w0 >> 8;
+      return (i & 1) ? value_f16((x & 0x00F000F0u) | F16_64, F16_NEG_64, p) : value_f16((x & 0x000F000Fu) | F16_1024, F16_NEG_1024, p);
+    }
+  }
+}
+template <int BITS, bool BF>
+__device__ __forceinline__ uint4 row_run(uint32_t w0, uint32_t w1, const PairScale& p) {   // eight channels
+  return make_uint4(row_pair<BITS, BF>(w0, w1, 0, p), row_pair<BITS, BF>(w0, w1, 1, p), row_pair<BITS, BF>(w0, w1, 2, p),
+                    row_pair<BITS, BF>(w0, w1, 3, p));
+}
+// Channel e (a constant, 0..7) of a run of eight in two rows, the first in the low half.  a, b: the rows' words (16 bits: four each; 8: two;
+// 4: one, of which the even channels of both rows are in `a` and the odd ones in `b`, see column_words).
+template <int BITS, bool BF>
+__device__ __forceinline__ uint32_t column_pair(const uint32_t* a, const uint32_t* b, int e, const PairScale& p) {
+  if constexpr (BITS == 16) {
+    return GEAR_BYTE_PERM(b[e >> 1], a[e >> 1], (e & 1) ? 0x07060302u : 0x05040100u);
+  } else if constexpr (BITS == 8) {
+    const uint32_t x = a[e >> 2], y = b[e >> 2];
+    const int k = e & 3;
+    if constexpr (BF) return value_bf16((x >> (8 * k)) & 0xFFu, (y >> (8 * k)) & 0xFFu, p);
+    else return value_f16(GEAR_BYTE_PERM(y, x, 0x0C040C00u + 0x00010001u * (uint32_t)k) | F16_1024, F16_NEG_1024, p);
+  } else {
+    const uint32_t w = (e & 1) ? b[0] : a[0];
+    const int i = e >> 1;
+    if constexpr (BF) {
+      return value_bf16((w >> (4 * i)) & 0xFu, (w >> (4 * i + 16)) & 0xFu, p);
+    } else {
+      const uint32_t x = i < 2 ? w : w >> 8;
+      return (i & 1) ? value_f16((x & 0x00F000F0u) | F16_64, F16_NEG_64, p) : value_f16((x & 0x000F000Fu) | F16_1024, F16_NEG_1024, p);
+    }
+  }
+}
+
+// ---- attention ------------------------------------------------------------------
+struct PageAttn {
+  PageGeom geom;
+  const int32_t* q_start;
+  const int32_t* kv_len;
+  const int32_t* table;
+  RowView q, out;
+  float* rec_o;      // [record rows][n_split][128] partial sums
+  float2* rec_ml;    // [record rows][n_split] (maximum, sum of weights), in units of log2
+  float scale_log2;  // scale * log2(e)
+  int32_t width;     // entries of a sequence's row of the table
+  int32_t n_seqs, n_tokens, gq, causal;
+  int32_t n_split;   // parts of the key axis, at most
+  int32_t few;       // columns (new tokens x gq) up to which page_attn_few_kernel has a sequence; 0: page_attn_many_kernel has them all
+  int32_t few_cols;  // record rows per sequence and head there
+  int32_t tiles;     // column tiles of page_attn_many_kernel, at most
+};
+constexpr int KEY_STEP = 32, MANY_COLS = 128, MANY_KEYS = 64;
+constexpr int FEW_PART = 256, MANY_PART = 512;   // tokens of a part, at least
+
+// The key axis of `keys` tokens in at most n_split parts of `unit` x some: tokens of a part, and how many there are (at least one).
+struct Parts {
+  int len, count;
+};
+__host__ __device__ inline Parts parts_of(int keys, int n_split, int least, int unit) {
+  int n = keys / least;
+  n = n < 1 ? 1 : (n > n_split ? n_split : n);
+  const int len = ((keys + n - 1) / n + unit - 1) / unit * unit;
+  return Parts{len, len > 0 ? (keys + len - 1) / len : 1};
+}
+struct SeqSpan {
+  int q0, nq, kv;
+};
+__device__ __forceinline__ SeqSpan seq_span(const PageAttn& a, int s) {   // nothing outside the arrays, whatever the device holds
+  const int q0 = a.q_start[s], q1 = a.q_start[s + 1], kv = a.kv_len[s];
+  SeqSpan r;
+  r.q0 = max(q0, 0);
+  r.nq = min(q1, a.n_tokens) - r.q0;
+  r.kv = (int)min((long long)max(kv, 0), (long long)a.width << a.geom.shift);
+  return r;
+}
+// tokens that row `row` (of the sequence's nq) sees
+__device__ __forceinline__ int row_sees(const PageAttn& a, const SeqSpan& s, int row) {
+  return a.causal ? max(0, min(s.kv, s.kv - s.nq + row + 1)) : s.kv;
+}
+
+// Greatest value / sum over the lanes of a column, l % 16 (Q16) or l % 32.
+template <bool Q16>
+__device__ __forceinline__ float col_max(float v) {
+  uint32_t a = __float_as_uint(v), b = a;
+  GEAR_LANE_SWAP32(a, b);
+  v = fmaxf(__uint_as_float(a), __uint_as_float(b));
+  if constexpr (Q16) {
+    a = b = __float_as_uint(v);
+    GEAR_LANE_SWAP16(a, b);
+    v = fmaxf(__uint_as_float(a), __uint_as_float(b));
+  }
+  return v;
+}
+template <bool Q16>
+__device__ __forceinline__ float col_sum(float v) {
+  uint32_t a = __float_as_uint(v), b = a;
+  GEAR_LANE_SWAP32(a, b);
+  v = __uint_as_float(a) + __uint_as_float(b);
+  if constexpr (Q16) {
+    a = b = __float_as_uint(v);
+    GEAR_LANE_SWAP16(a, b);
+    v = __uint_as_float(a) + __uint_as_float(b);
+  }
+  return v;
+}
+
+}  // namespace gear

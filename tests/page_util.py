@@ -1,0 +1,119 @@
+"""The paged cache in plain form, in 64 bits on the CPU, from its definition in include/gear.h: layout, quantizer, attention, and how
+far an implementation in the declared precisions may be off."""
+import math
+
+import torch
+
+D = 128
+DTYPES = (torch.float16, torch.bfloat16)
+
+
+def to_type(x, dtype):
+    """float64 values rounded to the type, once: through fp32 only where that is exact or rounds to the same side (torch's own way goes
+    through fp32: a value within half an fp32 step of a tie would be rounded twice)."""
+    y = x.to(torch.float32)
+    # round to odd: an inexact fp32 value gets its last bit set, so that the second rounding sees on which side it was
+    bits = y.view(torch.int32)
+    inexact = y.double() != x
+    toward = (y.double().abs() > x.abs()) & inexact               # rounded away: the truncated neighbour
+    bits = torch.where(toward, bits - 1, bits)
+    bits = torch.where(inexact & torch.isfinite(y), bits | 1, bits)
+    return bits.view(torch.float32).to(dtype)
+
+
+def quantise(x, bits, group, dtype):
+    """(codes, scale, zero) of rows [..., 128] (any float type): codes [..., 128] int64, the others [..., 128 / group] of the type."""
+    x = x.double().unflatten(-1, (D // group, group))
+    zero, top = x.amin(-1), x.amax(-1)
+    # the scale is defined through fp32: a difference and a quotient, each rounded
+    scale = ((top - zero).float() / torch.tensor(float(2 ** bits - 1))).to(dtype)
+    s = scale.double()
+    code = torch.where(s[..., None] > 0, (x - zero[..., None]) / torch.where(s > 0, s, 1.0)[..., None], 0.0).round().clamp(0, 2 ** bits - 1)
+    return code.flatten(-2).long(), scale, zero.to(dtype)
+
+
+def stored_values(code, scale, zero, group, dtype):
+    s, z = (t.double().repeat_interleave(group, -1) for t in (scale, zero))
+    return to_type(code.double() * s + z, dtype)
+
+
+def expected(x, bits, group, dtype):
+    """What rows read back as."""
+    return x if bits == 16 else stored_values(*quantise(x, bits, group, dtype), group, dtype)
+
+
+def block_bytes(bits, group, page):
+    return page * (D * bits // 8 + (0 if bits == 16 else 4 * D // group))
+
+
+def pack(x, bits, group, dtype):
+    """Block bytes [..., bytes] of rows [..., page, 128]."""
+    page = x.shape[-2]
+    if bits == 16:
+        return x.contiguous().view(torch.uint8).reshape(*x.shape[:-2], -1)
+    code, scale, zero = quantise(x, bits, group, dtype)
+    if bits == 8:
+        rows = code.to(torch.uint8)
+    else:
+        word = sum(code[..., e::8] << (4 * (e // 2) + 16 * (e % 2)) for e in range(8))            # [..., page, 16]
+        rows = torch.stack([(word >> (8 * k)) & 255 for k in range(4)], -1).to(torch.uint8)
+    words = torch.stack((scale, zero), -1).transpose(-3, -2).contiguous().view(torch.uint8)        # [..., G, page, 4]
+    lead = x.shape[:-2]
+    return torch.cat((rows.reshape(*lead, -1), words.reshape(*lead, -1)), -1)
+
+
+def unpack(blocks, bits, group, dtype, page):
+    """Rows [..., page, 128] that blocks [..., bytes] hold, as values of the type."""
+    rb = D * bits // 8
+    rows = blocks[..., :page * rb].reshape(*blocks.shape[:-1], page, rb).contiguous()
+    if bits == 16:
+        return rows.view(dtype)
+    if bits == 4:
+        by = rows.long()
+        word = by[..., 0::4] | by[..., 1::4] << 8 | by[..., 2::4] << 16 | by[..., 3::4] << 24
+        rows = torch.stack([(word >> (4 * (e // 2) + 16 * (e % 2))) & 15 for e in range(8)], -1).flatten(-2)
+    words = blocks[..., page * rb:].contiguous().view(dtype).reshape(*blocks.shape[:-1], D // group, page, 2).transpose(-3, -2)
+    return stored_values(rows.long(), words[..., 0], words[..., 1], group, dtype)
+
+
+def attend(q, K, V, q_start, kv_len, table, scale, causal):
+    """(out, bound) in 64 bits: q [T, H_q, 128]; K, V [pages, H, page, 128] the pool's values; lists of ints.  Rows outside every sequence
+    are NaN in both.  bound: how far an output of the declared precisions may be from out."""
+    T, Hq, _ = q.shape
+    n_pages, H, page, _ = K.shape
+    gq, dtype = Hq // H, q.dtype
+    eps = torch.finfo(dtype).eps / 2
+    out = torch.full((T, Hq, D), math.nan, dtype=torch.float64)
+    bound = torch.full((T, Hq, D), math.nan, dtype=torch.float64)
+    for s in range(len(kv_len)):
+        q0, q1 = q_start[s], q_start[s + 1]
+        n, kv = q1 - q0, max(0, min(kv_len[s], len(table[s]) * page))
+        if n <= 0:
+            continue
+        pos = torch.arange(kv)
+        pages = torch.tensor([table[s][p // page] for p in range(kv)], dtype=torch.long)
+        there = (pages >= 0) & (pages < n_pages)
+        at = torch.where(there, pages, 0)
+        k, v = (torch.where(there[:, None, None], X[at, :, pos % page].double(), 0.0) for X in (K, V))   # [kv, H, 128]
+        last = torch.full((n,), kv) if not causal else (kv - n + 1 + torch.arange(n))
+        ban = ~there[None, :] | (pos[None, :] >= last[:, None])                                          # [n, kv]
+        for j in range(Hq):
+            qq, kk, vv = q[q0:q1, j].double(), k[:, j // gq], v[:, j // gq]
+            # (what no row sees may be anything)
+            kk, vv = (torch.where(ban.all(0)[:, None], 0.0, t) for t in (kk, vv))
+            sc = (qq @ kk.t() * scale).masked_fill(ban, -math.inf)
+            top = sc.amax(-1, keepdim=True) if kv else torch.full((n, 1), -math.inf, dtype=torch.float64)
+            w = torch.where(ban, 0.0, torch.exp(sc - torch.where(torch.isfinite(top), top, 0.0)))
+            l = w.sum(-1, keepdim=True)
+            p = torch.where(l > 0, w / torch.where(l > 0, l, 1.0), 0.0)
+            o, A = p @ vv, p @ vv.abs()
+            # scores: 128 products summed in fp32, times the scale (two roundings), and the exponent's argument; a score off by x changes a weight
+            # and the sum by x each
+            ds = (abs(scale) * (qq.abs() @ kk.abs().t()) * 136 * 2.0 ** -24).masked_fill(ban, 0.0).amax(-1, keepdim=True) if kv else 0.0
+            # weights: rounded to the type for the product (relative eps; half the last subnormal step of fp16, against a sum of at least 1),
+            # exp2 and the sums of kv terms in fp32
+            rel = eps + 2 * ds + (kv + 64) * 2.0 ** -23
+            tiny = (kv * 2.0 ** -25 if dtype == torch.float16 else 0.0) * (vv.abs().amax(0) if kv else 0.0)
+            b = A * rel + tiny
+            out[q0:q1, j], bound[q0:q1, j] = o, b + eps * (o.abs() + b) + (2.0 ** -25 if dtype == torch.float16 else 0.0)
+    return out, bound

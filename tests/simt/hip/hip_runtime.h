@@ -128,6 +128,7 @@ struct Wave {
   pthread_barrier_t bar;
   uint64_t slot[64];
   _Float16 ma[64][8], mb[64][8];
+  float fa[64][8], fb[64][8];
 };
 extern Wave waves[16];
 extern pthread_barrier_t block_bar;
@@ -233,6 +234,65 @@ inline f4 mfma(h8 a, h8 b, f4 c) {
   pthread_barrier_wait(&w.bar);
   return d;
 }
+// The paged cache's products, in either 16-bit type: a lane's eight values as floats.  n = 16: as above; n = 32 (v_mfma_f32_32x32x16):
+// A lane L = row L%32, k = 8*(L/32)+0..7, B the same for columns, D lane L register i = row 8*(i/4)+4*(L/32)+i%4, col L%32.
+inline float value16(uint32_t bits, bool bf) {
+  if (bf) {
+    const uint32_t w = bits << 16;
+    float f;
+    memcpy(&f, &w, 4);
+    return f;
+  }
+  const uint16_t h = (uint16_t)bits;
+  _Float16 f;
+  memcpy(&f, &h, 2);
+  return (float)f;
+}
+template <int N, class V>
+inline V mfma_n(const uint4& a, const uint4& b, const V& c, bool bf) {
+  Wave& w = W();
+  const int l = lane(), side = l / N, k = N == 16 ? 32 : 16;
+  const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+  for (int e = 0; e < 8; ++e) {
+    w.fa[l][e] = value16(x[e >> 1] >> (16 * (e & 1)) & 0xFFFFu, bf);
+    w.fb[l][e] = value16(y[e >> 1] >> (16 * (e & 1)) & 0xFFFFu, bf);
+  }
+  pthread_barrier_wait(&w.bar);
+  V d = c;
+  for (int i = 0; i < N * N / 64; ++i) {
+    const int row = N == 16 ? 4 * side + i : 8 * (i >> 2) + 4 * side + (i & 3), col = l % N;
+    double s = 0;
+    for (int j = 0; j < k; ++j) s += (double)w.fa[row + N * (j >> 3)][j & 7] * (double)w.fb[col + N * (j >> 3)][j & 7];
+    d[i] = c[i] + (float)s;
+  }
+  pthread_barrier_wait(&w.bar);
+  return d;
+}
+// ds_read_b64_tr_b16: in each group of 16 lanes lane i addresses columns 4 (i % 4) .. of row i / 4 and gets column i
+inline uint2 lds_read_tr(const unsigned char* p) {
+  const int l = lane(), group = l & ~15, i = l & 15;
+  uint64_t v;
+  memcpy(&v, p, 8);
+  uint64_t r = 0;
+  for (int e = 0; e < 4; ++e) r |= ((xchg(v, group + 4 * e + i / 4) >> (16 * (i % 4))) & 0xFFFFull) << (16 * e);
+  return uint2{(uint32_t)r, (uint32_t)(r >> 32)};
+}
+inline uint32_t bf16_of(float f) {   // to nearest, halves to even
+  uint32_t u;
+  memcpy(&u, &f, 4);
+  if ((u & 0x7F800000u) == 0x7F800000u) return (u >> 16) | ((u & 0xFFFFu) ? 0x40u : 0u);
+  return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
+}
+inline uint32_t pk_fma_f16(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r = 0;
+  for (int i = 0; i < 2; ++i) {   // (exact in fp64, but for sums of terms more than 2^32 apart)
+    const _Float16 h = (_Float16)((double)value16(a >> (16 * i), false) * (double)value16(b >> (16 * i), false) + (double)value16(c >> (16 * i), false));
+    uint16_t u;
+    memcpy(&u, &h, 2);
+    r |= (uint32_t)u << (16 * i);
+  }
+  return r;
+}
 // v_mfma_f32_4x4x1_16B_f32: 16 blocks of 4 lanes; register i of lane L gets
 // c[i] + a(lane 4*(L/4) + i) * b(lane L)
 inline f4 mfma4x4x1(float a, float b, f4 c) {
@@ -280,6 +340,7 @@ inline void launch(const void* kernel, const char* name, dim3 grid, dim3 block, 
 #define GEAR_MERGE_16 3
 #define GEAR_MERGE_32 4
 #endif
+#define GEAR_PAGE_CUS 4           // the paged cache's attention in parts
 #ifndef GEAR_BLOCK_SLOTS
 #define GEAR_BLOCK_SLOTS 16       // and strips of two tiles and more
 #endif
@@ -287,6 +348,15 @@ inline void launch(const void* kernel, const char* name, dim3 grid, dim3 block, 
   __builtin_bit_cast(gear::floatx4, simt::mfma(__builtin_bit_cast(simt::h8, (a)), __builtin_bit_cast(simt::h8, (b)), __builtin_bit_cast(simt::f4, (c))))
 #define __builtin_amdgcn_mfma_f32_4x4x1f32(a, b, c, x, y, z) \
   __builtin_bit_cast(gear::floatx4, simt::mfma4x4x1((a), (b), __builtin_bit_cast(simt::f4, (c))))
+#define GEAR_NO_BF16_TYPE
+#define GEAR_MFMA16_F16(a, b, c) simt::mfma_n<16>((a), (b), (c), false)
+#define GEAR_MFMA16_BF16(a, b, c) simt::mfma_n<16>((a), (b), (c), true)
+#define GEAR_MFMA32_F16(a, b, c) simt::mfma_n<32>((a), (b), (c), false)
+#define GEAR_MFMA32_BF16(a, b, c) simt::mfma_n<32>((a), (b), (c), true)
+#define GEAR_LDS_READ_TR(p) simt::lds_read_tr(p)
+#define GEAR_EXP2(x) exp2f(x)
+#define GEAR_PACK_BF2(a, b) (simt::bf16_of(a) | simt::bf16_of(b) << 16)
+#define GEAR_PK_FMA_F16(a, b, c) simt::pk_fma_f16((a), (b), (c))
 #define __syncthreads() pthread_barrier_wait(&simt::block_bar)
 // shuffles inside segments of w lanes (w a power of two), as HIP defines them
 template <typename T> inline T __shfl(T v, int src, int w = 64) { return simt::shfl(v, (simt::lane() & ~(w - 1)) + (src & (w - 1))); }
