@@ -196,7 +196,8 @@ int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_by
   a.table = b.page_table;
   a.q = view_of(q);
   a.out = view_of(out);
-  a.scale_log2 = scale * 1.44269504088896340736f;
+  a.scale_log2 = std::fmax(std::fabs(scale) * 1.44269504088896340736f, 1e-37f);   // (a scale of 0: every score comes to less than a step of 2^0)
+  a.flip = scale < 0.0f ? 0x80008000u : 0u;
   a.width = b.table_width;
   a.n_seqs = b.n_seqs;
   a.n_tokens = b.n_tokens;

@@ -136,7 +136,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_attn_few_kernel(PageAttn 
       sees[n] = row_sees(a, sp, row);
       const unsigned char* p = a.q.data + 2 * ((int64_t)(sp.q0 + row) * a.q.token + (int64_t)(head * a.gq + j) * a.q.head);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) q[n][t] = *reinterpret_cast<const uint4*>(p + 2 * first_channel<BITS>(t, hh));
+      for (int t = 0; t < 4; ++t) q[n][t] = signed_query(*reinterpret_cast<const uint4*>(p + 2 * first_channel<BITS>(t, hh)), a.flip);
     }
   }
   const int all_see = row_sees(a, sp, 0);   // every column sees the keys before this one
@@ -150,12 +150,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_attn_few_kernel(PageAttn 
 #pragma unroll
     for (int t = 0; t < 8; ++t) o[n][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   }
-  const int32_t* table = a.table + (int64_t)s * a.width;
-  auto page_of = [&](int key) -> int {   // -1: no page
-    if (key >= k1) return -1;
-    const int p = table[key >> g.shift];
-    return p >= 0 && p < g.n_pages ? p : -1;
-  };
+  PageRow pages = page_row(a, s, k1);
   auto fetch = [&](KeyBlock<BITS>& x, int key, int p0, int p1) {   // (a key without a page reads page 0, and counts for nothing)
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
@@ -168,7 +163,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_attn_few_kernel(PageAttn 
   };
   const int stride = KEY_STEP * (int)(blockDim.x >> 6);
   for (int key = k0 + KEY_STEP * wave; key < k1; key += stride) {
-    const int p0 = GEAR_WAVE_UNIFORM(page_of(key)), p1 = GEAR_WAVE_UNIFORM(page_of(key + 16));
+    const int p0 = page_of(pages, key), p1 = page_of(pages, key + 16);
     KeyBlock<BITS> x;
     fetch(x, key, p0, p1);
     // scores: keys 4 hh + 0..3 of each 16, column c
@@ -200,11 +195,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_attn_few_kernel(PageAttn 
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          score[n][b][i] *= a.scale_log2;
           if (edge && ((b == 0 ? p0 : p1) < 0 || key + 16 * b + 4 * hh + i >= sees[n])) score[n][b][i] = -INFINITY;
           top = fmaxf(top, score[n][b][i]);
         }
-      top = col_max<true>(top);
+      top = col_max<true>(top) * a.scale_log2;
       if (__ballot(top > m[n]) != 0ull) {
         const float now = fmaxf(m[n], top), by = now == -INFINITY ? 1.0f : GEAR_EXP2(m[n] - now);
         m[n] = now;
@@ -218,7 +212,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_attn_few_kernel(PageAttn 
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          p[4 * b + i] = GEAR_EXP2(score[n][b][i] - from);
+          p[4 * b + i] = GEAR_EXP2(__builtin_fmaf(score[n][b][i], a.scale_log2, -from));
           l[n] += p[4 * b + i];
         }
       // rounded to the type for the product (2^-11 or 2^-8 of each weight, as the outputs are); the sum keeps them in fp32

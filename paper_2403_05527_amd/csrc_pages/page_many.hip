@@ -82,7 +82,7 @@ __device__ __forceinline__ void stage_store(const Staged<BITS>& x, unsigned char
 }
 
 template <int BITS, bool BF>
-__global__ __launch_bounds__(MANY_THREADS) void page_attn_many_kernel(PageAttn a) {
+__global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_many_kernel(PageAttn a) {
   GEAR_DYN_LDS(lds);   // [two tiles][Keys, Values][64 rows]
   const PageGeom& g = a.geom;
   const int lane = lane_id(), wave = GEAR_WAVE_UNIFORM((int)(threadIdx.x >> 6)), c = lane & 31, half = lane >> 5;
@@ -116,22 +116,25 @@ __global__ __launch_bounds__(MANY_THREADS) void page_attn_many_kernel(PageAttn a
   if (mine) {
     const unsigned char* p = a.q.data + 2 * ((int64_t)(sp.q0 + row) * a.q.token + (int64_t)(head * a.gq + j) * a.q.head + 8 * half);
 #pragma unroll
-    for (int t = 0; t < 8; ++t) q[t] = *reinterpret_cast<const uint4*>(p + 32 * t);
+    for (int t = 0; t < 8; ++t) q[t] = signed_query(*reinterpret_cast<const uint4*>(p + 32 * t), a.flip);
   }
   const int all_see = row_sees(a, sp, min(col0 + 32 * wave, cols - 1) / a.gq);   // every column of the wave sees the keys before this one
 
-  const int32_t* table = a.table + (int64_t)s * a.width;
-  auto page_of = [&](int key) -> int {   // -1: no page
-    if (key >= k1) return -1;
-    const int p = table[key >> g.shift];
-    return p >= 0 && p < g.n_pages ? p : -1;
-  };
+  PageRow pages = page_row(a, s, k1);
   Staged<BITS> next;
-  int live = 0;   // the wave's rows of `next` that there are
+  int live = 0, have = 0, have_next = 0;   // the wave's rows of `next` that there are; bit w: the tile's keys from 16 w on have a page
   auto fetch = [&](int key) {
-    const int at = key + 16 * wave, p = GEAR_WAVE_UNIFORM(page_of(at));
-    live = p < 0 ? 0 : min(16, k1 - at);
-    const unsigned char* block = g.pool + (uint64_t)(p < 0 ? 0 : p) * g.page_bytes + (uint64_t)(2 * head) * g.block_bytes;
+    int mine_page = 0;
+    have_next = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const int p = page_of(pages, key + 16 * w);
+      have_next |= (p >= 0 ? 1 : 0) << w;
+      if (w == wave) mine_page = p;
+    }
+    const int at = key + 16 * wave;
+    live = mine_page < 0 ? 0 : min(16, k1 - at);
+    const unsigned char* block = g.pool + (uint64_t)max(mine_page, 0) * g.page_bytes + (uint64_t)(2 * head) * g.block_bytes;
     stage_load<BITS>(next, g, block, (uint32_t)at & page_mask(g), lane);
   };
   floatx16 o[4];
@@ -148,6 +151,7 @@ __global__ __launch_bounds__(MANY_THREADS) void page_attn_many_kernel(PageAttn a
   int buf = 0;
   for (int key = k0; key < k1; key += MANY_KEYS, buf ^= 1) {
     const bool more = key + MANY_KEYS < k1;
+    have = have_next;
     if (more) fetch(key + MANY_KEYS);
     const unsigned char* kt = lds + buf * 2 * TILE_BYTES;
     const unsigned char* vt = kt + TILE_BYTES;
@@ -164,23 +168,14 @@ __global__ __launch_bounds__(MANY_THREADS) void page_attn_many_kernel(PageAttn a
         }
       }
       // keys 32 b + 8 (i / 4) + 4 half + i % 4 of the tile
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sc[b][i] *= a.scale_log2;
-      bool edge = key + MANY_KEYS > all_see;
-      int pages = 0;   // bit w: the 16 keys from 16 w on have a page
-#pragma unroll
-      for (int w = 0; w < 4; ++w) pages |= (page_of(key + 16 * w) >= 0 ? 1 : 0) << w;
-      pages = GEAR_WAVE_UNIFORM(pages);
-      edge = edge || pages != 15;
+      const bool edge = key + MANY_KEYS > all_see || have != 15;
       if (edge) {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int at = 32 * b + 8 * (i >> 2) + 4 * half + (i & 3);
-            if (key + at >= sees || ((pages >> (2 * b + (i >> 3))) & 1) == 0) sc[b][i] = -INFINITY;
+            if (key + at >= sees || ((have >> (2 * b + (i >> 3))) & 1) == 0) sc[b][i] = -INFINITY;
           }
       }
       float top = -INFINITY;
@@ -189,6 +184,7 @@ __global__ __launch_bounds__(MANY_THREADS) void page_attn_many_kernel(PageAttn a
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[b][i]);
       top = col_max<false>(top);
+      top *= a.scale_log2;
       if (__ballot(top > m + MANY_SLACK) != 0ull) {   // (from -inf on: any score)
         const float now = fmaxf(m, top), by = now == -INFINITY ? 1.0f : GEAR_EXP2(m - now);
         m = now;
@@ -203,7 +199,7 @@ __global__ __launch_bounds__(MANY_THREADS) void page_attn_many_kernel(PageAttn a
         float p[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          p[i] = GEAR_EXP2(sc[u >> 1][8 * (u & 1) + i] - from);
+          p[i] = GEAR_EXP2(__builtin_fmaf(sc[u >> 1][8 * (u & 1) + i], a.scale_log2, -from));
           l += p[i];
         }
         // rounded to the type for the product (2^-11 or 2^-8 of each weight, as the outputs are); the sum keeps them in fp32

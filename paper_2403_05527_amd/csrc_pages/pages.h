@@ -177,7 +177,8 @@ struct PageAttn {
   RowView q, out;
   float* rec_o;      // [record rows][n_split][128] partial sums
   float2* rec_ml;    // [record rows][n_split] (maximum, sum of weights), in units of log2
-  float scale_log2;  // scale * log2(e)
+  float scale_log2;  // |scale| * log2(e), above 0: scores are compared before they are scaled, and -inf times it is -inf
+  uint32_t flip;     // 0x80008000 where the scale is negative: the queries change sign instead
   int32_t width;     // entries of a sequence's row of the table
   int32_t n_seqs, n_tokens, gq, causal;
   int32_t n_split;   // parts of the key axis, at most
@@ -214,6 +215,28 @@ __device__ __forceinline__ int row_sees(const PageAttn& a, const SeqSpan& s, int
   return a.causal ? max(0, min(s.kv, s.kv - s.nq + row + 1)) : s.kv;
 }
 
+// A sequence's row of the page table as a wave reads it: 64 entries at a time, one per lane, so that a step waits for the table once per 64
+// pages and not for each.
+struct PageRow {
+  const int32_t* table;
+  int32_t base, held, n_pages, shift, end;   // `end`: no key from there on is asked for
+};
+__device__ __forceinline__ PageRow page_row(const PageAttn& a, int s, int end) {
+  return PageRow{a.table + (int64_t)s * a.width, -64, 0, a.geom.n_pages, a.geom.shift, end};
+}
+// The page of a key (the same in all lanes of the wave); -1: none.  Keys are asked for in ascending order.
+__device__ __forceinline__ int page_of(PageRow& r, int key) {
+  if (key >= r.end) return -1;
+  const int i = key >> r.shift;
+  if (i >= r.base + 64) {
+    r.base = i;
+    const int at = i + lane_id(), last = (r.end - 1) >> r.shift;
+    const int p = r.table[at <= last ? at : last];
+    r.held = p >= 0 && p < r.n_pages ? p : -1;
+  }
+  return __builtin_amdgcn_readlane(r.held, i - r.base);
+}
+__device__ __forceinline__ uint4 signed_query(const uint4& q, uint32_t flip) { return make_uint4(q.x ^ flip, q.y ^ flip, q.z ^ flip, q.w ^ flip); }
 // Greatest value / sum over the lanes of a column, l % 16 (Q16) or l % 32.
 template <bool Q16>
 __device__ __forceinline__ float col_max(float v) {
