@@ -5,10 +5,11 @@
 // whose index has bit 2 equal to its half; both products take the keys in that order, so the weights go from the softmax to the
 // second product without leaving the registers, and maximum and sum are one exchange between the halves.  The tile's
 // rows lie in LDS as 16-bit values (codes are converted once per block, on their way in): Key operands are 16-byte reads,
-// Value operands transposing reads of 4 rows x 16 channels.  Rows are 256 bytes, and their 16-byte pieces are stored at
-// (piece ^ row % 16) for Keys, (piece ^ 2 (row % 8)) for Values: the eight lanes, resp. the eight rows of two pieces, that
-// one cycle of a read serves then lie in different banks.
-// Two tiles: the next one's global loads run while this one is worked on.
+// Value operands transposing reads of 4 rows x 16 channels.  A row's sixteen 16-byte pieces are stored at (piece ^ row % 16) for Keys, so
+// that the 16 rows which a read serves at a time lie in different banks, and at (piece ^ 4 (row % 4)) for Values, whose reads serve four rows of four
+// pieces at a time (with 2 (row % 8): every read twice as long).
+// Two tiles: the next one's rows are requested once this one's scores are under way (copied straight into LDS at 16 bits; the
+// compiler lets no LDS read pass a copy that is on its way, so a request at the top of the step would be waited for at once).
 //
 // The maximum that the weights are taken from is raised only when a score exceeds it by more than 8 (in powers of two): weights are
 // then at most 256, exact enough in either type, and the 64 accumulators are rarely rescaled.
@@ -21,7 +22,7 @@ constexpr float MANY_SLACK = 8.0f;
 constexpr int TILE_BYTES = MANY_KEYS * D * 2;
 
 __device__ __forceinline__ uint32_t key_at(uint32_t row, uint32_t piece) { return row * 256 + ((piece ^ (row & 15)) << 4); }
-__device__ __forceinline__ uint32_t value_at(uint32_t row, uint32_t piece) { return row * 256 + ((piece ^ ((row & 7) << 1)) << 4); }
+__device__ __forceinline__ uint32_t value_at(uint32_t row, uint32_t piece) { return row * 256 + ((piece ^ ((row & 3) << 2)) << 4); }
 
 // A wave's 16 rows of the next tile on their way: 128 / BITS channels per lane and load.
 template <int BITS>
@@ -121,21 +122,36 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_many_kernel(PageAtt
   const int all_see = row_sees(a, sp, min(col0 + 32 * wave, cols - 1) / a.gq);   // every column of the wave sees the keys before this one
 
   PageRow pages = page_row(a, s, k1);
-  Staged<BITS> next;
-  int live = 0, have = 0, have_next = 0;   // the wave's rows of `next` that there are; bit w: the tile's keys from 16 w on have a page
-  auto fetch = [&](int key) {
-    int mine_page = 0;
+  Staged<BITS> next;                       // codes on their way
+  int live = 0, have = 0, have_next = 0;   // of the next tile: the wave's rows that there are; bit w: the keys from 16 w on have a page
+  auto fetch = [&](int key, unsigned char* to) {
+    // (the entries of the tile's four groups of 16 keys lie within four of each other: one look at what the wave holds)
+    const int i0 = key >> g.shift;
+    if (i0 + 4 > pages.base + 64) load_entries(pages, i0);
+    const int at = key + 16 * wave, left = k1 - key;
+    int page = 0;
     have_next = 0;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const int p = page_of(pages, key + 16 * w);
-      have_next |= (p >= 0 ? 1 : 0) << w;
-      if (w == wave) mine_page = p;
+      const int p = __builtin_amdgcn_readlane(pages.held, ((key + 16 * w) >> g.shift) - pages.base);
+      have_next |= (p >= 0 && 16 * w < left ? 1 : 0) << w;
+      page = w == wave ? p : page;
     }
-    const int at = key + 16 * wave;
-    live = mine_page < 0 ? 0 : min(16, k1 - at);
-    const unsigned char* block = g.pool + (uint64_t)max(mine_page, 0) * g.page_bytes + (uint64_t)(2 * head) * g.block_bytes;
-    stage_load<BITS>(next, g, block, (uint32_t)at & page_mask(g), lane);
+    live = page < 0 ? 0 : min(16, max(0, k1 - at));
+    const unsigned char* block = g.pool + (uint64_t)max(page, 0) * g.page_bytes + (uint64_t)(2 * head) * g.block_bytes;
+    const uint32_t row0 = (uint32_t)at & page_mask(g);
+    if (BITS == 16 && live == 16) {   // straight into LDS: 16 lanes per row, each the piece that belongs at its place
+      const auto kb = GEAR_BUF_MAKE(block + row0 * 256, 16 * 256), vb = GEAR_BUF_MAKE(block + g.block_bytes + row0 * 256, 16 * 256);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t row = 4 * i + (lane >> 4);
+        GEAR_DMA16(kb, key_at(row, lane & 15), to + 4096 * wave + 1024 * i);
+        GEAR_DMA16(vb, value_at(row, lane & 15), to + TILE_BYTES + 4096 * wave + 1024 * i);
+      }
+    } else {
+      stage_load<BITS>(next, g, block, row0, lane);
+      if (BITS == 16) stage_store<BITS, BF>(next, to, to + TILE_BYTES, wave, lane, live);   // (a sequence's last rows)
+    }
   };
   floatx16 o[4];
 #pragma unroll
@@ -144,19 +160,19 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_many_kernel(PageAtt
     for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
   float m = -INFINITY, l = 0.0f;
   if (k0 < k1) {
-    fetch(k0);
-    stage_store<BITS, BF>(next, lds, lds + TILE_BYTES, wave, lane, live);
+    fetch(k0, lds);
+    if (BITS < 16) stage_store<BITS, BF>(next, lds, lds + TILE_BYTES, wave, lane, live);
   }
-  block_lds_sync();
+  GEAR_DMA_WAIT();
+  GEAR_DMA_BARRIER();
   int buf = 0;
   for (int key = k0; key < k1; key += MANY_KEYS, buf ^= 1) {
     const bool more = key + MANY_KEYS < k1;
     have = have_next;
-    if (more) fetch(key + MANY_KEYS);
     const unsigned char* kt = lds + buf * 2 * TILE_BYTES;
     const unsigned char* vt = kt + TILE_BYTES;
+    floatx16 sc[2];
     if (busy) {
-      floatx16 sc[2];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
 #pragma unroll
@@ -167,6 +183,9 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_many_kernel(PageAtt
           sc[b] = mfma32<BF>(ka, q[t], sc[b]);
         }
       }
+    }
+    if (more) fetch(key + MANY_KEYS, lds + (buf ^ 1) * 2 * TILE_BYTES);
+    if (busy) {
       // keys 32 b + 8 (i / 4) + 4 half + i % 4 of the tile
       const bool edge = key + MANY_KEYS > all_see || have != 15;
       if (edge) {
@@ -218,9 +237,10 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_many_kernel(PageAtt
     }
     if (more) {
       unsigned char* to = lds + (buf ^ 1) * 2 * TILE_BYTES;
-      stage_store<BITS, BF>(next, to, to + TILE_BYTES, wave, lane, live);
+      if (BITS < 16) stage_store<BITS, BF>(next, to, to + TILE_BYTES, wave, lane, live);
     }
-    block_lds_sync();
+    GEAR_DMA_WAIT();
+    GEAR_DMA_BARRIER();
   }
   if (!busy) return;
   l = col_sum<false>(l);

@@ -224,16 +224,17 @@ struct PageRow {
 __device__ __forceinline__ PageRow page_row(const PageAttn& a, int s, int end) {
   return PageRow{a.table + (int64_t)s * a.width, -64, 0, a.geom.n_pages, a.geom.shift, end};
 }
+__device__ __forceinline__ void load_entries(PageRow& r, int i) {   // from entry i on, which is one of a key before `end`; behind the last: that one
+  r.base = i;
+  const int at = i + lane_id(), last = (r.end - 1) >> r.shift;
+  const int p = r.table[at <= last ? at : last];
+  r.held = p >= 0 && p < r.n_pages ? p : -1;
+}
 // The page of a key (the same in all lanes of the wave); -1: none.  Keys are asked for in ascending order.
 __device__ __forceinline__ int page_of(PageRow& r, int key) {
   if (key >= r.end) return -1;
   const int i = key >> r.shift;
-  if (i >= r.base + 64) {
-    r.base = i;
-    const int at = i + lane_id(), last = (r.end - 1) >> r.shift;
-    const int p = r.table[at <= last ? at : last];
-    r.held = p >= 0 && p < r.n_pages ? p : -1;
-  }
+  if (i >= r.base + 64) load_entries(r, i);
   return __builtin_amdgcn_readlane(r.held, i - r.base);
 }
 __device__ __forceinline__ uint4 signed_query(const uint4& q, uint32_t flip) { return make_uint4(q.x ^ flip, q.y ^ flip, q.z ^ flip, q.w ^ flip); }
