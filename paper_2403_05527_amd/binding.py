@@ -228,36 +228,41 @@ def make_page_config(n_pages, page_size, H_kv, bits, group=128, dtype=torch.floa
     return gear_page_config(n_pages, page_size, H_kv, d_h, bits, group, GEAR_DTYPES[dtype])
 
 
-def _here(t, what):
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
-        raise ValueError("%s lies on %s, not on the current GPU" % (what, t.device))
+def _page_device():
+    """The current GPU's index; where none is in use yet, one that no tensor lies on."""
+    if not torch.cuda.is_initialized():
+        return -2
+    return torch.cuda.current_device() if _device is None else _device()
 
 
-def _page_rows(t, cfg, heads, what):
+# (One pass over what a call is given, 1 us a tensor: a decode step's kernels take 6 to 10.)
+def _page_rows(t, cfg, heads, device, what):
     """(the view, sequences, tokens) of a tensor of rows."""
-    if t.dim() not in (3, 4) or t.shape[-1] != cfg.d_h or t.shape[-2] != heads:
-        raise ValueError("%s is [n_seqs, tokens, %d, %d] or without the first: got %s" % (what, heads, cfg.d_h, tuple(t.shape)))
-    if GEAR_DTYPES.get(t.dtype) != cfg.dtype or t.stride(-1) != 1:
+    shape, stride = t.shape, t.stride()
+    n = len(shape)
+    if n not in (3, 4) or shape[-1] != cfg.d_h or shape[-2] != heads:
+        raise ValueError("%s is [n_seqs, tokens, %d, %d] or without the first: got %s" % (what, heads, cfg.d_h, tuple(shape)))
+    if GEAR_DTYPES.get(t.dtype) != cfg.dtype or stride[-1] != 1:
         raise ValueError("%s: another type than the pool's, or a row that is not contiguous" % what)
-    _here(t, what)
-    s = t.stride()
-    if t.dim() == 3:
-        return gear_page_rows(t.data_ptr(), 0, s[0], s[1]), 1, t.shape[0]
-    return gear_page_rows(t.data_ptr(), s[0], s[1], s[2]), t.shape[0], t.shape[1]
+    if t.get_device() != device:
+        raise ValueError("%s lies on %s, not on the current GPU" % (what, t.device))
+    if n == 3:
+        return gear_page_rows(t.data_ptr(), 0, stride[0], stride[1]), 1, shape[0]
+    return gear_page_rows(t.data_ptr(), stride[0], stride[1], stride[2]), shape[0], shape[1]
 
 
-def _page_index(t, dtype, n, what):
+def _page_index(t, dtype, n, device, what):
     if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
         raise ValueError("%s is a contiguous %s tensor of %d entries: got %s %s" % (what, dtype, n, t.dtype, tuple(t.shape)))
-    _here(t, what)
+    if t.get_device() != device:
+        raise ValueError("%s lies on %s, not on the current GPU" % (what, t.device))
     return t.data_ptr()
 
 
-def _page_pool(pool):
-    if not pool.is_contiguous():
-        raise ValueError("the pool is one contiguous tensor")
-    _here(pool, "the pool")
-    return pool.data_ptr(), _bytes(pool)
+def _page_bytes(t, device, what):
+    if t.get_device() != device or not t.is_contiguous():
+        raise ValueError("%s is one contiguous tensor on the current GPU: got one on %s" % (what, t.device))
+    return t.data_ptr(), t.nbytes
 
 
 def gear_page_bytes(cfg):
@@ -267,16 +272,17 @@ def gear_page_bytes(cfg):
 
 
 def _page_copy(name, cfg, pool, K, V, slots):
-    k, v = (None if t is None else _page_rows(t, cfg, cfg.H_kv, w) for t, w in ((K, "K"), (V, "V")))
-    some = k or v
-    if some is None:
+    device = _page_device()
+    k = None if K is None else _page_rows(K, cfg, cfg.H_kv, device, "K")
+    v = None if V is None else _page_rows(V, cfg, cfg.H_kv, device, "V")
+    if k is None and v is None:
         raise ValueError("neither K nor V is given")
     if k and v and k[1:] != v[1:]:
         raise ValueError("K and V differ in their rows: %s and %s" % (tuple(K.shape), tuple(V.shape)))
-    p, n = _page_pool(pool)
-    at = _page_index(slots, torch.int64, some[1] * some[2], "slots")
-    _check(getattr(load_library(), name)(ctypes.byref(cfg), p, n, k and ctypes.byref(k[0]), v and ctypes.byref(v[0]), some[1], some[2], at,
-                                         _stream()), name)
+    _, n_seqs, n_rows = k or v
+    p, n = _page_bytes(pool, device, "the pool")
+    _check(getattr(load_library(), name)(cfg, p, n, k and k[0], v and v[0], n_seqs, n_rows,
+                                         _page_index(slots, torch.int64, n_seqs * n_rows, device, "slots"), _stream()), name)
 
 
 def gear_page_write(cfg, pool, K, V, slots):
@@ -291,8 +297,9 @@ def make_page_batch(q_start, kv_len, page_table, n_tokens, max_q, max_kv, causal
     """The batch of a gear_page_attn call (one serves all layers of a step): int32 tensors q_start [n_seqs + 1], kv_len [n_seqs],
     page_table [n_seqs, width].  It keeps them alive."""
     n, width = page_table.shape
-    b = gear_page_batch(n, n_tokens, max_q, max_kv, width, 1 if causal else 0, _page_index(q_start, torch.int32, n + 1, "q_start"),
-                        _page_index(kv_len, torch.int32, n, "kv_len"), _page_index(page_table, torch.int32, n * width, "page_table"))
+    d = _page_device()
+    b = gear_page_batch(n, n_tokens, max_q, max_kv, width, 1 if causal else 0, _page_index(q_start, torch.int32, n + 1, d, "q_start"),
+                        _page_index(kv_len, torch.int32, n, d, "kv_len"), _page_index(page_table, torch.int32, n * width, d, "page_table"))
     b.tensors = (q_start, kv_len, page_table)
     return b
 
@@ -304,14 +311,15 @@ def gear_page_attn_bytes(cfg, H_q, batch):
 
 
 def gear_page_attn(cfg, pool, batch, q, out, scale, workspace):
+    device = _page_device()
     H_q = q.shape[-2]
-    a, b = _page_rows(q, cfg, H_q, "q"), _page_rows(out, cfg, H_q, "out")
-    if q.dim() != 3 or out.dim() != 3 or a[2] != batch.n_tokens or b[2] != batch.n_tokens:
+    a, seqs, n = _page_rows(q, cfg, H_q, device, "q")
+    b, seqs_out, n_out = _page_rows(out, cfg, H_q, device, "out")
+    if not seqs * n == seqs_out * n_out == n == n_out == batch.n_tokens:
         raise ValueError("q and out are [%d, H_q, %d]: got %s and %s" % (batch.n_tokens, cfg.d_h, tuple(q.shape), tuple(out.shape)))
-    p, n = _page_pool(pool)
-    w, wn = (None, 0) if workspace is None else _page_pool(workspace)
-    _check(load_library().gear_page_attn(ctypes.byref(cfg), p, n, ctypes.byref(batch), ctypes.byref(a[0]), H_q, scale, ctypes.byref(b[0]), w,
-                                         wn, _stream()), "gear_page_attn")
+    p, size = _page_bytes(pool, device, "the pool")
+    w, w_size = (None, 0) if workspace is None else _page_bytes(workspace, device, "the workspace")
+    _check(load_library().gear_page_attn(cfg, p, size, batch, a, H_q, scale, b, w, w_size, _stream()), "gear_page_attn")
 
 
 # ---- convenience owner of the device buffers -------------------------------
