@@ -4,37 +4,58 @@
 
 namespace gear {
 
-// How the key axis is divided.  Blocks of either kernel that the chip holds at once; the axis is divided until there are about
-// as many, in parts of at least FEW_PART / MANY_PART tokens.
 #ifndef GEAR_PAGE_CUS   // (the CPU stand-in sets it, so that its small cases are divided)
 #define GEAR_PAGE_CUS GEAR_CUS
 #endif
-constexpr int FEW_SLOTS = 3 * GEAR_PAGE_CUS, MANY_SLOTS = 2 * GEAR_PAGE_CUS;
 constexpr int FEW_COLS_MOST = 32;
+// Blocks of the few-column kernel that the chip holds at once, with one tile of columns; records' rows x parts are bounded by twice that.
+constexpr int FEW_SLOTS = 2 * GEAR_PAGE_CUS, FEW_BLOCKS_MOST = 2 * FEW_SLOTS, MANY_SLOTS = 2 * GEAR_PAGE_CUS;
 
-static int split_by(int64_t blocks, int slots, int max_kv, int least) {
-  const int by_keys = max_kv / least, by_slots = blocks > 0 ? (int)(slots / blocks) : 1;
-  const int n = by_keys < by_slots ? by_keys : by_slots;
-  return n < 1 ? 1 : n;
+// Parts of the key axis for `blocks` (sequence, head) pairs of up to max_kv tokens and `cols` columns: the best number of equal parts by a
+// model in ns.  A block takes 4000 (its launch, the first loads, the joining of its waves) and 8 per token (the chain of a wave's steps, by eight
+// waves); all of them together no less than their bytes at 6 TB/s; with more than one part the merge takes 3500, the launch of a wave per four records and their bytes
+// at 5 TB/s.  1 x 8 heads x 32768 tokens at 4 bits: 21.2 us in 96 parts of 341 tokens, 18.3 in 64 with the merge, 19.6 in 32; 33 sequences x 8 heads of 600 to 4000
+// tokens: 46 us undivided, 41 and 15 of merging in three parts.
+static int few_parts(int64_t blocks, int cols, int max_kv, int bytes_per_key, int slots) {
+  const int by_keys = max_kv / FEW_PART;
+  const int64_t by_blocks = blocks > 0 ? FEW_BLOCKS_MOST / blocks : 1;
+  const int most = (int)(by_blocks < by_keys ? by_blocks : by_keys);
+  const double bytes = (double)blocks * max_kv * bytes_per_key / 6000.0;
+  int best = 1;
+  double least = 0.0;
+  for (int n = 1; n <= most; ++n) {
+    const double chain = (double)((blocks * n + slots - 1) / slots) * (4000.0 + 8.0 * max_kv / n);
+    const double t = (chain > bytes ? chain : bytes) + (n > 1 ? 3500.0 + 20.0 * n + (double)blocks * cols * n * 1040.0 / 5000.0 : 0.0);
+    if (n == 1 || t < least) {
+      best = n;
+      least = t;
+    }
+  }
+  return best;
 }
 
-PagePlan page_plan(int H, int gq, int n_seqs, int n_tokens, int max_q, int max_kv) {
+PagePlan page_plan(int H, int gq, int n_seqs, int n_tokens, int max_q, int max_kv, int bytes_per_key) {
   PagePlan p{};
   const int64_t cols = (int64_t)max_q * gq;
   const bool all_few = cols <= FEW_COLS_MOST;
-  // (a batch that is not n_seqs x max_q has shorter sequences, single tokens for instance)
-  p.few = all_few || ((int64_t)n_seqs * max_q != n_tokens && gq <= FEW_COLS_MOST);
+  // (a batch that is not n_seqs x max_q has shorter sequences, single tokens for instance: one tile of columns is theirs, if it holds one)
+  const bool uniform = (int64_t)n_seqs * max_q == n_tokens;
+  p.few = all_few || (!uniform && gq <= FEW_COLS_MOST);
   p.many = !all_few;
-  p.few_limit = p.few ? (all_few ? (int)cols : FEW_COLS_MOST) : 0;
+  p.few_limit = !p.few ? 0 : all_few ? (int)cols : gq <= 16 ? 16 : FEW_COLS_MOST;
   p.few_tiles = p.few_limit <= 16 ? 1 : 2;
   p.few_split = p.many_split = 1;
   if (p.few) {
-    p.few_split = split_by((int64_t)n_seqs * H, FEW_SLOTS, max_kv, FEW_PART);
+    p.few_split = few_parts((int64_t)n_seqs * H, p.few_limit, max_kv, bytes_per_key, p.few_tiles == 1 ? FEW_SLOTS : FEW_SLOTS / 2);
     if (p.few_split > 1) p.few_rows = (int64_t)n_seqs * H * p.few_limit;
   }
   if (p.many) {
-    const int64_t tiles = ((int64_t)n_tokens * gq + MANY_COLS - 1) / MANY_COLS;
-    p.many_split = split_by(tiles * H, MANY_SLOTS, max_kv, MANY_PART);
+    // As many parts as fill the slots once.  Not more, even where the sequences differ: three chunks of 483 to 566 tokens behind up to 2900, 416 blocks,
+    // take 100 us in one part each and 140 in two, of which 18 go to joining the records (35 MB each way).
+    const int64_t blocks = ((int64_t)n_tokens * gq + MANY_COLS - 1) / MANY_COLS * H, by_slots = blocks > 0 ? MANY_SLOTS / blocks : 1;
+    const int64_t by_keys = max_kv / MANY_PART, n = by_slots < by_keys ? by_slots : by_keys;
+    p.many_split = n < 1 ? 1 : (int)n;
+    p.many_least = max_kv / p.many_split > MANY_PART ? max_kv / p.many_split : MANY_PART;
     if (p.many_split > 1) p.many_rows = (int64_t)n_tokens * H * gq;
   }
   return p;
@@ -45,7 +66,7 @@ int64_t page_records_most(int H, int gq, int n_seqs, int n_tokens, int max_q, in
   const int64_t few_cols = (int64_t)max_q * gq < FEW_COLS_MOST ? (int64_t)max_q * gq : FEW_COLS_MOST;
   int64_t few = 0, many = 0;
   if (max_kv / FEW_PART > 1) {
-    const int64_t by_keys = (int64_t)n_seqs * H * (max_kv / FEW_PART), blocks = by_keys < FEW_SLOTS ? by_keys : FEW_SLOTS;
+    const int64_t by_keys = (int64_t)n_seqs * H * (max_kv / FEW_PART), blocks = by_keys < FEW_BLOCKS_MOST ? by_keys : FEW_BLOCKS_MOST;
     few = blocks * few_cols;
   }
   if ((int64_t)max_q * gq > FEW_COLS_MOST && max_kv / MANY_PART > 1) {
@@ -182,7 +203,8 @@ int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_by
   if (misaligned(b.q_start, 4) || misaligned(b.kv_len, 4) || misaligned(b.page_table, 4) || misaligned(workspace, 16)) return GEAR_EALIGN;
   if ((int64_t)b.table_width * cfg->page_size > INT_MOST - 1024) return GEAR_ECAPACITY;
   const int H = cfg->H_kv, gq = H_q / H;
-  const PagePlan p = page_plan(H, gq, b.n_seqs, b.n_tokens, b.max_q, b.max_kv);
+  const int per_key = 2 * (int)(a.geom.block_bytes >> a.geom.shift);
+  const PagePlan p = page_plan(H, gq, b.n_seqs, b.n_tokens, b.max_q, b.max_kv, per_key);
   const int64_t few_recs = p.few_rows * p.few_split, many_recs = p.many_rows * p.many_split;
   if (few_recs + many_recs > 0) {
     if (!workspace) return GEAR_EINVAL;
@@ -212,6 +234,7 @@ int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_by
   if (p.many) {   // the longer kernel first
     PageAttn m = a;
     m.n_split = p.many_split;
+    m.least = p.many_least;
     m.rec_o = rec;
     m.rec_ml = reinterpret_cast<float2*>(rec + many_recs * D);
     if (launch_page_many(m, cfg->bits, bf, st) != hipSuccess) return GEAR_EHIP;
@@ -219,6 +242,7 @@ int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_by
   if (p.few) {
     PageAttn f = a;
     f.n_split = p.few_split;
+    f.least = FEW_PART;
     f.rec_o = rec + many_recs * (D + 2);
     f.rec_ml = reinterpret_cast<float2*>(f.rec_o + few_recs * D);
     if (launch_page_few(f, cfg->bits, bf, p.few_tiles, st) != hipSuccess) return GEAR_EHIP;

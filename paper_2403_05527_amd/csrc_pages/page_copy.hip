@@ -74,7 +74,7 @@ __device__ __forceinline__ uint4 load_piece(const PageGeom& g, const unsigned ch
     uint2 w = make_uint2(0, 0);
     if constexpr (BITS == 8) w = *reinterpret_cast<const uint2*>(block + (r * 16 + c) * 8);
     else w.x = *reinterpret_cast<const uint32_t*>(block + (r * 16 + c) * 4);
-    return row_run<BITS, BF>(w.x, w.y, pair_scale<BF>(sz, sz));
+    return row_run<BITS, BF>(w.x, w.y, pair_scale<BF>(sz, sz), biases());
   }
 }
 

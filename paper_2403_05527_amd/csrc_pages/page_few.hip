@@ -15,7 +15,7 @@
 
 namespace gear {
 
-constexpr int FEW_WAVES = 4;
+constexpr int FEW_WAVES = 8;
 
 // 16 keys' rows of one head as loaded.
 template <int BITS>
@@ -31,30 +31,46 @@ __device__ __forceinline__ int first_channel(int t, int hh) {
   constexpr int PER = PIECE / 8;                 // products per piece
   return (t / PER) * 4 * PIECE + hh * PIECE + (t % PER) * 8;
 }
+// A lane's places in 16 rows: Keys of row c = l % 16, Values of rows 4 hh + 0..3, hh = l / 16; relative to the first row and its words.
 template <int BITS>
-__device__ __forceinline__ void load_keys(KeyRows<BITS>& k, const PageGeom& g, const unsigned char* block, uint32_t row, int hh) {
-  const unsigned char* p = block + row * g.row_bytes + hh * 16;
-#pragma unroll
-  for (int u = 0; u < KeyRows<BITS>::LOADS; ++u) k.w[u] = *reinterpret_cast<const uint4*>(p + 64 * u);
+struct LaneOffsets {
+  uint32_t key, value, key_word[BITS == 8 ? 2 : 1], value_word;
+};
+template <int BITS>
+__device__ __forceinline__ LaneOffsets<BITS> lane_offsets(const PageGeom& g, int c, int hh) {
+  LaneOffsets<BITS> o{};
+  o.key = c * (16 * BITS) + hh * 16;
+  o.value = 4 * hh * (16 * BITS) + c * BITS;
   if constexpr (BITS < 16) {
-    const uint32_t* words = reinterpret_cast<const uint32_t*>(block + words_at(g));
 #pragma unroll
-    for (int u = 0; u < KeyRows<BITS>::LOADS; ++u)
-      k.sz[u] = words[((uint32_t)(first_channel<BITS>(u * (16 / BITS), hh) >> g.gshift) << g.shift) + row];
+    for (int u = 0; u < KeyRows<BITS>::LOADS; ++u) o.key_word[u] = 4 * (((uint32_t)(first_channel<BITS>(u * (16 / BITS), hh) >> g.gshift) << g.shift) + c);
+    o.value_word = 4 * (((uint32_t)((8 * c) >> g.gshift) << g.shift) + 4 * hh);
+  }
+  return o;
+}
+template <int BITS>
+__device__ __forceinline__ void load_keys(KeyRows<BITS>& k, const PageGeom& g, const unsigned char* block, uint32_t row0, const LaneOffsets<BITS>& o) {
+  const auto rows = GEAR_BUF_MAKE(block + row0 * (16 * BITS), 16 * (16 * BITS));
+#pragma unroll
+  for (int u = 0; u < KeyRows<BITS>::LOADS; ++u) k.w[u] = GEAR_BUF_LOAD16(rows, o.key + 64 * u);
+  if constexpr (BITS < 16) {
+    const auto words = GEAR_BUF_MAKE(block + words_at(g) + row0 * 4, g.block_bytes - words_at(g) - row0 * 4);
+#pragma unroll
+    for (int u = 0; u < KeyRows<BITS>::LOADS; ++u) k.sz[u] = GEAR_BUF_LOAD4(words, o.key_word[u]);
   }
 }
 template <int BITS, bool BF>
-__device__ __forceinline__ uint4 key_operand(const KeyRows<BITS>& k, int t) {
+__device__ __forceinline__ uint4 key_operand(const KeyRows<BITS>& k, int t, const Biases& bs) {
   if constexpr (BITS == 16) {
     return k.w[t];
   } else if constexpr (BITS == 8) {
     const uint4& w = k.w[t >> 1];
     const PairScale p = pair_scale<BF>(k.sz[t >> 1], k.sz[t >> 1]);
-    return (t & 1) ? row_run<8, BF>(w.z, w.w, p) : row_run<8, BF>(w.x, w.y, p);
+    return (t & 1) ? row_run<8, BF>(w.z, w.w, p, bs) : row_run<8, BF>(w.x, w.y, p, bs);
   } else {
     const uint4& w = k.w[0];
     const PairScale p = pair_scale<BF>(k.sz[0], k.sz[0]);
-    return row_run<4, BF>(t == 0 ? w.x : t == 1 ? w.y : t == 2 ? w.z : w.w, 0u, p);
+    return row_run<4, BF>(t == 0 ? w.x : t == 1 ? w.y : t == 2 ? w.z : w.w, 0u, p, bs);
   }
 }
 // Eight channels of four consecutive rows.
@@ -65,26 +81,27 @@ struct ValueRows {
   uint32_t sz[4];
 };
 template <int BITS>
-__device__ __forceinline__ void load_values(ValueRows<BITS>& v, const PageGeom& g, const unsigned char* block, uint32_t row, int c) {
-  const unsigned char* p = block + row * g.row_bytes + c * BITS;
+__device__ __forceinline__ void load_values(ValueRows<BITS>& v, const PageGeom& g, const unsigned char* block, uint32_t row0, const LaneOffsets<BITS>& o) {
+  const auto rows = GEAR_BUF_MAKE(block + row0 * (16 * BITS), 16 * (16 * BITS));
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if constexpr (BITS == 16) {
-      const uint4 x = *reinterpret_cast<const uint4*>(p + i * 256);
+      const uint4 x = GEAR_BUF_LOAD16(rows, o.value + i * 256);
       v.w[i][0] = x.x;
       v.w[i][1] = x.y;
       v.w[i][2] = x.z;
       v.w[i][3] = x.w;
     } else if constexpr (BITS == 8) {
-      const uint2 x = *reinterpret_cast<const uint2*>(p + i * 128);
+      const uint2 x = GEAR_BUF_LOAD8(rows, o.value + i * 128);
       v.w[i][0] = x.x;
       v.w[i][1] = x.y;
     } else {
-      v.w[i][0] = *reinterpret_cast<const uint32_t*>(p + i * 64);
+      v.w[i][0] = GEAR_BUF_LOAD4(rows, o.value + i * 64);
     }
   }
-  if constexpr (BITS < 16) {   // (rows 4 hh .. of a page of 16 and more: 16-byte aligned)
-    const uint4 x = *reinterpret_cast<const uint4*>(block + words_at(g) + 4 * (((uint32_t)((8 * c) >> g.gshift) << g.shift) + row));
+  if constexpr (BITS < 16) {   // (four rows of a page of 16 and more: 16-byte aligned)
+    const auto words = GEAR_BUF_MAKE(block + words_at(g) + row0 * 4, g.block_bytes - words_at(g) - row0 * 4);
+    const uint4 x = GEAR_BUF_LOAD16(words, o.value_word);
     v.sz[0] = x.x;
     v.sz[1] = x.y;
     v.sz[2] = x.z;
@@ -97,13 +114,6 @@ __device__ __forceinline__ void drop_value(ValueRows<BITS>& v, int i) {   // a r
   for (int j = 0; j < ValueRows<BITS>::WORDS; ++j) v.w[i][j] = 0u;
   v.sz[i] = 0u;
 }
-// (the even channels of two rows in the first word, the odd ones in the second: what column_pair wants of 4-bit rows)
-__device__ __forceinline__ void column_words(uint32_t& a, uint32_t& b) {
-  const uint32_t x = a, y = b;
-  a = GEAR_BYTE_PERM(y, x, 0x05040100u);
-  b = GEAR_BYTE_PERM(y, x, 0x07060302u);
-}
-
 template <int BITS>
 struct KeyBlock {   // 32 keys
   KeyRows<BITS> k[2];
@@ -119,7 +129,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_attn_few_kernel(PageAttn 
   const SeqSpan sp = seq_span(a, s);
   const int cols = sp.nq * a.gq;
   if (sp.nq <= 0 || sp.nq > a.few || cols > a.few) return;
-  const Parts parts = parts_of(sp.kv, a.n_split, FEW_PART, KEY_STEP);
+  const Parts parts = parts_of(sp.kv, a.n_split, a.least, KEY_STEP);
   if (part >= parts.count) return;
   const int k0 = part * parts.len, k1 = min(sp.kv, k0 + parts.len);
 
@@ -151,17 +161,19 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_attn_few_kernel(PageAttn 
     for (int t = 0; t < 8; ++t) o[n][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   }
   PageRow pages = page_row(a, s, k1);
+  const Biases bs = biases();
+  const LaneOffsets<BITS> offsets = lane_offsets<BITS>(g, c, hh);
   auto fetch = [&](KeyBlock<BITS>& x, int key, int p0, int p1) {   // (a key without a page reads page 0, and counts for nothing)
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const int p = b == 0 ? p0 : p1;
       const unsigned char* block = g.pool + (uint64_t)(p < 0 ? 0 : p) * g.page_bytes + (uint64_t)(2 * head) * g.block_bytes;
-      const uint32_t row = (uint32_t)(key + 16 * b) & page_mask(g);
-      load_keys<BITS>(x.k[b], g, block, row + c, hh);
-      load_values<BITS>(x.v[b], g, block + g.block_bytes, row + 4 * hh, c);
+      const uint32_t row0 = (uint32_t)(key + 16 * b) & page_mask(g);
+      load_keys<BITS>(x.k[b], g, block, row0, offsets);
+      load_values<BITS>(x.v[b], g, block + g.block_bytes, row0, offsets);
     }
   };
-  const int stride = KEY_STEP * (int)(blockDim.x >> 6);
+  const int stride = KEY_STEP * FEW_WAVES;
   for (int key = k0 + KEY_STEP * wave; key < k1; key += stride) {
     const int p0 = page_of(pages, key), p1 = page_of(pages, key + 16);
     KeyBlock<BITS> x;
@@ -174,18 +186,26 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_attn_few_kernel(PageAttn 
       for (int n = 0; n < NC; ++n) score[n][b] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const uint4 ka = key_operand<BITS, BF>(x.k[b], t);
+        const uint4 ka = key_operand<BITS, BF>(x.k[b], t, bs);
 #pragma unroll
         for (int n = 0; n < NC; ++n) score[n][b] = mfma16<BF>(ka, q[n][t], score[n][b]);
       }
     }
-    const bool edge = key + KEY_STEP > all_see || p0 < 0 || p1 < 0;
+    const bool edge = key + KEY_STEP > all_see || p0 < 0 || p1 < 0;   // some column does not see some of the keys
     if (edge) {
+      int first = key + 4 * hh;
+      GEAR_PIN_VGPR(first);   // (what depends on it stays in here: as selections on `edge` every step would pay for it)
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if ((b == 0 ? p0 : p1) < 0 || key + 16 * b + 4 * hh + i >= sp.kv) drop_value<BITS>(x.v[b], i);
+        for (int i = 0; i < 4; ++i) {
+          const int at = first + 16 * b + i;
+          const bool there = (b == 0 ? p0 : p1) >= 0;
+          if (!there || at >= sp.kv) drop_value<BITS>(x.v[b], i);
+#pragma unroll
+          for (int n = 0; n < NC; ++n)
+            if (!there || at >= sees[n]) score[n][b][i] = -INFINITY;
+        }
     }
     uint4 pw[NC];
 #pragma unroll
@@ -195,7 +215,6 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_attn_few_kernel(PageAttn 
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (edge && ((b == 0 ? p0 : p1) < 0 || key + 16 * b + 4 * hh + i >= sees[n])) score[n][b][i] = -INFINITY;
           top = fmaxf(top, score[n][b][i]);
         }
       top = col_max<true>(top) * a.scale_log2;
@@ -218,12 +237,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_attn_few_kernel(PageAttn 
       // rounded to the type for the product (2^-11 or 2^-8 of each weight, as the outputs are); the sum keeps them in fp32
       pw[n] = make_uint4(pack2<BF>(p[0], p[1]), pack2<BF>(p[2], p[3]), pack2<BF>(p[4], p[5]), pack2<BF>(p[6], p[7]));
     }
-    if constexpr (BITS == 4) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        column_words(x.v[b].w[0][0], x.v[b].w[1][0]);
-        column_words(x.v[b].w[2][0], x.v[b].w[3][0]);
-      }
+    for (int b = 0; b < 2; ++b) {
+      column_words<BITS>(x.v[b].w[0], x.v[b].w[1]);
+      column_words<BITS>(x.v[b].w[2], x.v[b].w[3]);
     }
     PairScale ps[4];
     if constexpr (BITS < 16) {
@@ -238,8 +255,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_attn_few_kernel(PageAttn 
       uint32_t w[4];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        w[2 * b] = column_pair<BITS, BF>(x.v[b].w[0], x.v[b].w[1], t, ps[2 * b]);
-        w[2 * b + 1] = column_pair<BITS, BF>(x.v[b].w[2], x.v[b].w[3], t, ps[2 * b + 1]);
+        w[2 * b] = column_pair<BITS, BF>(x.v[b].w[0], x.v[b].w[1], t, ps[2 * b], bs);
+        w[2 * b + 1] = column_pair<BITS, BF>(x.v[b].w[2], x.v[b].w[3], t, ps[2 * b + 1], bs);
       }
       const uint4 va = make_uint4(w[0], w[1], w[2], w[3]);
 #pragma unroll
@@ -248,7 +265,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_attn_few_kernel(PageAttn 
   }
 
   // the waves' states: every wave brings its own to the common maximum, then sums and stores a share of the channels
-  const int waves = (int)(blockDim.x >> 6);
+  constexpr int waves = FEW_WAVES;
   float* top_of = reinterpret_cast<float*>(lds);                   // [wave][NC * 16]
   float* sum_of = top_of + waves * NC * 16;
   float4* part_of = reinterpret_cast<float4*>(sum_of + waves * NC * 16);
@@ -312,7 +329,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_merge_few_kernel(PageAttn
   const SeqSpan sp = seq_span(a, s);
   const int cols = sp.nq * a.gq;
   if (sp.nq <= 0 || sp.nq > a.few || cols > a.few || col >= cols) return;
-  const Parts parts = parts_of(sp.kv, a.n_split, FEW_PART, KEY_STEP);
+  const Parts parts = parts_of(sp.kv, a.n_split, a.least, KEY_STEP);
   if (parts.count <= 1) return;
   const int lane = lane_id(), wave = (int)(threadIdx.x >> 6);
   const int64_t rec = (((int64_t)s * g.H + head) * a.few_cols + col) * a.n_split;
@@ -321,12 +338,21 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_merge_few_kernel(PageAttn
   top = wave_max(top);
   const float from = top == -INFINITY ? 0.0f : top;
   float sum = 0.0f, x = 0.0f, y = 0.0f;
-  for (int i = wave; i < parts.count; i += FEW_WAVES) {
-    const float2 ml = a.rec_ml[rec + i], v = *reinterpret_cast<const float2*>(a.rec_o + (rec + i) * D + 2 * lane);
-    const float by = GEAR_EXP2(ml.x - from);
-    sum += ml.y * by;
-    x += v.x * by;
-    y += v.y * by;
+  for (int i0 = wave; i0 < parts.count; i0 += FEW_WAVES * 8) {   // eight records on their way at a time
+    float2 ml[8], v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int64_t i = rec + min(i0 + FEW_WAVES * u, parts.count - 1);
+      ml[u] = a.rec_ml[i];
+      v[u] = *reinterpret_cast<const float2*>(a.rec_o + i * D + 2 * lane);
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float by = i0 + FEW_WAVES * u < parts.count ? GEAR_EXP2(ml[u].x - from) : 0.0f;
+      sum += ml[u].y * by;
+      x += v[u].x * by;
+      y += v[u].y * by;
+    }
   }
   float* sh = reinterpret_cast<float*>(lds);   // [wave][3][lane]
   sh[(wave * 3 + 0) * 64 + lane] = sum;

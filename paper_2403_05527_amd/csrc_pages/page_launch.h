@@ -15,9 +15,10 @@ struct PagePlan {
   int few_limit;            // columns up to which a sequence counts as of few
   int few_tiles;            // column tiles of 16 of the few-column kernel (1 or 2)
   int few_split, many_split;
+  int many_least;           // tokens of a part, about, where the keys are divided
   int64_t few_rows, many_rows;   // record rows (times the parts), 0 where there is one part
 };
-PagePlan page_plan(int H, int gq, int n_seqs, int n_tokens, int max_q, int max_kv);
+PagePlan page_plan(int H, int gq, int n_seqs, int n_tokens, int max_q, int max_kv, int bytes_per_key);   // bytes: of a token in one head
 // record rows x parts that no batch within these bounds exceeds
 int64_t page_records_most(int H, int gq, int n_seqs, int n_tokens, int max_q, int max_kv);
 

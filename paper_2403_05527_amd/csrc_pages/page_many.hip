@@ -49,14 +49,14 @@ __device__ __forceinline__ void stage_load(Staged<BITS>& x, const PageGeom& g, c
   }
 }
 template <int BITS, bool BF>
-__device__ __forceinline__ uint4 staged_run(const uint4& w, int j, const PairScale& p) {   // channels 8 j .. of the lane's piece
+__device__ __forceinline__ uint4 staged_run(const uint4& w, int j, const PairScale& p, const Biases& bs) {   // channels 8 j .. of the lane's piece
   if constexpr (BITS == 16) return w;
-  else if constexpr (BITS == 8) return j == 0 ? row_run<8, BF>(w.x, w.y, p) : row_run<8, BF>(w.z, w.w, p);
-  else return row_run<4, BF>(j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w, 0u, p);
+  else if constexpr (BITS == 8) return j == 0 ? row_run<8, BF>(w.x, w.y, p, bs) : row_run<8, BF>(w.z, w.w, p, bs);
+  else return row_run<4, BF>(j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w, 0u, p, bs);
 }
 // into LDS; `live`: the wave's rows from there on are zeroes as Values, whatever the page holds (their weights are 0)
 template <int BITS, bool BF>
-__device__ __forceinline__ void stage_store(const Staged<BITS>& x, unsigned char* kt, unsigned char* vt, int wave, int lane, int live) {
+__device__ __forceinline__ void stage_store(const Staged<BITS>& x, unsigned char* kt, unsigned char* vt, int wave, int lane, int live, const Biases& bs) {
   using S = Staged<BITS>;
   const uint32_t piece = lane % S::LANES;
 #pragma unroll
@@ -71,8 +71,8 @@ __device__ __forceinline__ void stage_store(const Staged<BITS>& x, unsigned char
 #pragma unroll
     for (int j = 0; j < S::PIECE / 8; ++j) {
       const uint32_t at = piece * (S::PIECE / 8) + j;
-      *reinterpret_cast<uint4*>(kt + key_at(row, at)) = staged_run<BITS, BF>(x.k[i], j, pk);
-      uint4 v = staged_run<BITS, BF>(x.v[i], j, pv);
+      *reinterpret_cast<uint4*>(kt + key_at(row, at)) = staged_run<BITS, BF>(x.k[i], j, pk, bs);
+      uint4 v = staged_run<BITS, BF>(x.v[i], j, pv, bs);
       v.x = there ? v.x : 0u;
       v.y = there ? v.y : 0u;
       v.z = there ? v.z : 0u;
@@ -82,29 +82,61 @@ __device__ __forceinline__ void stage_store(const Staged<BITS>& x, unsigned char
   }
 }
 
+// Tile `i` of the call's column tiles (s < 0: there is none).
+struct ColTile {
+  int s, col0;
+};
+__device__ __forceinline__ int many_tiles(const PageAttn& a, const SeqSpan& sp) {   // of a sequence
+  if (sp.nq <= 0 || (sp.nq <= a.few && sp.nq * a.gq <= a.few)) return 0;
+  return (sp.nq * a.gq + MANY_COLS - 1) / MANY_COLS;
+}
+// The tiles that see the most keys come first: sequences by their length, and a sequence's last tiles before its first (with the longest of three
+// sequences last, a batch took half as long again).  Each lane counts, for one sequence, the tiles of those that come before it.  More than 64
+// sequences: in their order.
+__device__ __forceinline__ ColTile col_tile(const PageAttn& a, int i, int lane) {
+  if (a.n_seqs <= 64) {
+    SeqSpan sp{0, 0, 0};
+    if (lane < a.n_seqs) sp = seq_span(a, lane);
+    const int tiles = many_tiles(a, sp);
+    int before = 0;
+    for (int j = 0; j < a.n_seqs; ++j) {
+      const int kv = __builtin_amdgcn_readlane(sp.kv, j), n = __builtin_amdgcn_readlane(tiles, j);
+      before += kv > sp.kv || (kv == sp.kv && j < lane) ? n : 0;
+    }
+    const unsigned long long mine = __ballot(i >= before && i < before + tiles);
+    if (mine == 0ull) return ColTile{-1, 0};
+    const int s = GEAR_WAVE_UNIFORM(__ffsll((long long)mine) - 1);
+    return ColTile{s, (__builtin_amdgcn_readlane(before + tiles, s) - 1 - i) * MANY_COLS};
+  }
+  // sequence s has the tiles from q_start[s] * gq / 128 + s on: room for its own last, partly filled one
+  const int tile = a.tiles - 1 - i;
+  int s = -1;
+  for (int base = 0; base < a.n_seqs; base += 64) {
+    const int j = base + lane;
+    s += __popcll(__ballot(j < a.n_seqs && ((long long)max(a.q_start[j], 0) * a.gq) / MANY_COLS + j <= tile));
+  }
+  s = GEAR_WAVE_UNIFORM(s);
+  if (s < 0) return ColTile{-1, 0};
+  const SeqSpan sp = seq_span(a, s);
+  const int local = tile - (int)(((long long)sp.q0 * a.gq) / MANY_COLS + s);
+  return local >= 0 && local < many_tiles(a, sp) ? ColTile{s, local * MANY_COLS} : ColTile{-1, 0};
+}
+
 template <int BITS, bool BF>
 __global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_many_kernel(PageAttn a) {
   GEAR_DYN_LDS(lds);   // [two tiles][Keys, Values][64 rows]
   const PageGeom& g = a.geom;
   const int lane = lane_id(), wave = GEAR_WAVE_UNIFORM((int)(threadIdx.x >> 6)), c = lane & 31, half = lane >> 5;
-  // heads next to each other: with 8 of them and more, a head's tiles share one XCD's L2.  Later tiles, which see more keys, first.
-  const int bid = (int)blockIdx.x, head = bid % g.H, rest = bid / g.H, part = rest % a.n_split, tile = a.tiles - 1 - rest / a.n_split;
-  // sequence s has the tiles from q_start[s] * gq / 128 + s on: room for its own last, partly filled one
-  int s = -1;
-  for (int base = 0; base < a.n_seqs; base += 64) {
-    const int i = base + lane;
-    const bool before = i < a.n_seqs && ((long long)max(a.q_start[i], 0) * a.gq) / MANY_COLS + i <= tile;
-    s += __popcll(__ballot(before));
-  }
-  s = GEAR_WAVE_UNIFORM(s);
-  if (s < 0) return;
+  // heads next to each other: with 8 of them and more, a head's tiles share one XCD's L2
+  const int bid = (int)blockIdx.x, head = bid % g.H, rest = bid / g.H, part = rest % a.n_split;
+  const ColTile ct = col_tile(a, rest / a.n_split, lane);
+  if (ct.s < 0) return;
+  const int s = ct.s, col0 = ct.col0;
   const SeqSpan sp = seq_span(a, s);
-  if (sp.nq <= 0) return;
-  const int cols = sp.nq * a.gq, col0 = (tile - ((int)(((long long)sp.q0 * a.gq) / MANY_COLS) + s)) * MANY_COLS;
-  if (col0 < 0 || col0 >= cols || (sp.nq <= a.few && cols <= a.few)) return;
+  const int cols = sp.nq * a.gq;
   const int last = min(col0 + MANY_COLS, cols) - 1;
   const int keys = row_sees(a, sp, last / a.gq);
-  const Parts parts = parts_of(keys, a.n_split, MANY_PART, MANY_KEYS);
+  const Parts parts = parts_of(keys, a.n_split, a.least, MANY_KEYS);
   if (part >= parts.count) return;
   const int k0 = part * parts.len, k1 = min(keys, k0 + parts.len);
 
@@ -122,6 +154,7 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_many_kernel(PageAtt
   const int all_see = row_sees(a, sp, min(col0 + 32 * wave, cols - 1) / a.gq);   // every column of the wave sees the keys before this one
 
   PageRow pages = page_row(a, s, k1);
+  const Biases bs = biases();
   Staged<BITS> next;                       // codes on their way
   int live = 0, have = 0, have_next = 0;   // of the next tile: the wave's rows that there are; bit w: the keys from 16 w on have a page
   auto fetch = [&](int key, unsigned char* to) {
@@ -150,7 +183,7 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_many_kernel(PageAtt
       }
     } else {
       stage_load<BITS>(next, g, block, row0, lane);
-      if (BITS == 16) stage_store<BITS, BF>(next, to, to + TILE_BYTES, wave, lane, live);   // (a sequence's last rows)
+      if (BITS == 16) stage_store<BITS, BF>(next, to, to + TILE_BYTES, wave, lane, live, bs);   // (a sequence's last rows)
     }
   };
   floatx16 o[4];
@@ -161,7 +194,7 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_many_kernel(PageAtt
   float m = -INFINITY, l = 0.0f;
   if (k0 < k1) {
     fetch(k0, lds);
-    if (BITS < 16) stage_store<BITS, BF>(next, lds, lds + TILE_BYTES, wave, lane, live);
+    if (BITS < 16) stage_store<BITS, BF>(next, lds, lds + TILE_BYTES, wave, lane, live, bs);
   }
   GEAR_DMA_WAIT();
   GEAR_DMA_BARRIER();
@@ -189,12 +222,13 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_many_kernel(PageAtt
       // keys 32 b + 8 (i / 4) + 4 half + i % 4 of the tile
       const bool edge = key + MANY_KEYS > all_see || have != 15;
       if (edge) {
+        int first = key + 4 * half;
+        GEAR_PIN_VGPR(first);   // (what depends on it stays in here)
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int at = 32 * b + 8 * (i >> 2) + 4 * half + (i & 3);
-            if (key + at >= sees || ((have >> (2 * b + (i >> 3))) & 1) == 0) sc[b][i] = -INFINITY;
+            if (first + 32 * b + 8 * (i >> 2) + (i & 3) >= sees || ((have >> (2 * b + (i >> 3))) & 1) == 0) sc[b][i] = -INFINITY;
           }
       }
       float top = -INFINITY;
@@ -237,7 +271,7 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_many_kernel(PageAtt
     }
     if (more) {
       unsigned char* to = lds + (buf ^ 1) * 2 * TILE_BYTES;
-      if (BITS < 16) stage_store<BITS, BF>(next, to, to + TILE_BYTES, wave, lane, live);
+      if (BITS < 16) stage_store<BITS, BF>(next, to, to + TILE_BYTES, wave, lane, live, bs);
     }
     GEAR_DMA_WAIT();
     GEAR_DMA_BARRIER();
@@ -285,7 +319,7 @@ __global__ __launch_bounds__(256) void page_merge_many_kernel(PageAttn a, int bf
   const int row = token - sp.q0, cols = sp.nq * a.gq;
   if (row < 0 || row >= sp.nq || (sp.nq <= a.few && cols <= a.few)) return;
   const int col = row * a.gq + (jq - head * a.gq), last = min(col / MANY_COLS * MANY_COLS + MANY_COLS, cols) - 1;
-  const Parts parts = parts_of(row_sees(a, sp, last / a.gq), a.n_split, MANY_PART, MANY_KEYS);
+  const Parts parts = parts_of(row_sees(a, sp, last / a.gq), a.n_split, a.least, MANY_KEYS);
   if (parts.count <= 1) return;
   const int64_t rec = id * a.n_split;
   float top = -INFINITY;

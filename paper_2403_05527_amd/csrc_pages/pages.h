@@ -37,6 +37,11 @@
                                                          __builtin_bit_cast(gear::h2_t, (c))))
 #endif
 
+// A constant that is kept in a vector register (an instruction that takes two constants can have one from a scalar register only).
+#ifndef GEAR_IN_VGPR
+#define GEAR_IN_VGPR(x) asm("" : "+v"(x))
+#endif
+
 namespace gear {
 
 typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
@@ -111,7 +116,17 @@ __device__ __forceinline__ PairScale pair_scale(uint32_t sz0, uint32_t sz1) {
   }
   return p;
 }
-constexpr uint32_t F16_1024 = 0x64006400u, F16_64 = 0x54005400u, F16_NEG_1024 = 0xE400E400u, F16_NEG_64 = 0xD400D400u;
+// 1024 and 64 in both halves, where one instruction puts masked codes into them.
+struct Biases {
+  uint32_t b1024, b64;
+};
+__device__ __forceinline__ Biases biases() {
+  Biases b{0x64006400u, 0x54005400u};
+  GEAR_IN_VGPR(b.b1024);
+  GEAR_IN_VGPR(b.b64);
+  return b;
+}
+constexpr uint32_t BYTES_64H = 0x64646464u, F16_NEG_1024 = 0xE400E400u, F16_NEG_64 = 0xD400D400u;
 // fp16: value pair of (1024 + code) or (64 + code) pairs.  Both steps are exact but for the one rounding of the fused multiply-add:
 // the value that a code stands for.
 __device__ __forceinline__ uint32_t value_f16(uint32_t biased, uint32_t neg_bias, const PairScale& p) {
@@ -123,48 +138,51 @@ __device__ __forceinline__ uint32_t value_bf16(uint32_t c0, uint32_t c1, const P
 }
 // Channels 2 i, 2 i + 1 (i = 0..3) of a run of eight along a row: w0, w1 are the run's code words (w1 at 8 bits only).
 template <int BITS, bool BF>
-__device__ __forceinline__ uint32_t row_pair(uint32_t w0, uint32_t w1, int i, const PairScale& p) {
+__device__ __forceinline__ uint32_t row_pair(uint32_t w0, uint32_t w1, int i, const PairScale& p, const Biases& bs) {
   if constexpr (BITS == 8) {
     const uint32_t w = i < 2 ? w0 : w1;
     if constexpr (BF) {
       return value_bf16((w >> (16 * (i & 1))) & 0xFFu, (w >> (16 * (i & 1) + 8)) & 0xFFu, p);
     } else {
-      return value_f16(GEAR_BYTE_PERM(F16_1024 | 0x00640064u, w, (i & 1) ? 0x04030402u : 0x04010400u), F16_NEG_1024, p);
+      return value_f16(GEAR_BYTE_PERM(BYTES_64H, w, (i & 1) ? 0x04030402u : 0x04010400u), F16_NEG_1024, p);
     }
   } else {   // 4 bits: nibble i of each half
     if constexpr (BF) {
       return value_bf16((w0 >> (4 * i)) & 0xFu, (w0 >> (4 * i + 16)) & 0xFu, p);
     } else {
       const uint32_t x = i < 2 ? w0 : w0 >> 8;
-      return (i & 1) ? value_f16((x & 0x00F000F0u) | F16_64, F16_NEG_64, p) : value_f16((x & 0x000F000Fu) | F16_1024, F16_NEG_1024, p);
+      return (i & 1) ? value_f16((x & 0x00F000F0u) | bs.b64, F16_NEG_64, p) : value_f16((x & 0x000F000Fu) | bs.b1024, F16_NEG_1024, p);
     }
   }
 }
 template <int BITS, bool BF>
-__device__ __forceinline__ uint4 row_run(uint32_t w0, uint32_t w1, const PairScale& p) {   // eight channels
-  return make_uint4(row_pair<BITS, BF>(w0, w1, 0, p), row_pair<BITS, BF>(w0, w1, 1, p), row_pair<BITS, BF>(w0, w1, 2, p),
-                    row_pair<BITS, BF>(w0, w1, 3, p));
+__device__ __forceinline__ uint4 row_run(uint32_t w0, uint32_t w1, const PairScale& p, const Biases& bs) {   // eight channels
+  return make_uint4(row_pair<BITS, BF>(w0, w1, 0, p, bs), row_pair<BITS, BF>(w0, w1, 1, p, bs), row_pair<BITS, BF>(w0, w1, 2, p, bs),
+                    row_pair<BITS, BF>(w0, w1, 3, p, bs));
 }
-// Channel e (a constant, 0..7) of a run of eight in two rows, the first in the low half.  a, b: the rows' words (16 bits: four each; 8: two;
-// 4: one, of which the even channels of both rows are in `a` and the odd ones in `b`, see column_words).
+// Two rows' words of eight channels (16 bits: four each; 8: two; 4: one), brought into the order that column_pair takes from them.
+// 8 bits: the rows' bytes of two channels in each word (x: channels 0, 1 and 4, 5; y: 2, 3 and 6, 7), the first row's first; 4 bits: the rows'
+// even channels in x, the odd ones in y.
+template <int BITS>
+__device__ __forceinline__ void column_words(uint32_t* x, uint32_t* y) {
+#pragma unroll
+  for (int j = 0; j < (BITS == 16 ? 0 : BITS / 4); ++j) {
+    const uint32_t a = x[j], b = y[j];
+    x[j] = GEAR_BYTE_PERM(b, a, BITS == 8 ? 0x05010400u : 0x05040100u);
+    y[j] = GEAR_BYTE_PERM(b, a, BITS == 8 ? 0x07030602u : 0x07060302u);
+  }
+}
+// Channel e (a constant, 0..7) of the two rows, the first in the low half.
 template <int BITS, bool BF>
-__device__ __forceinline__ uint32_t column_pair(const uint32_t* a, const uint32_t* b, int e, const PairScale& p) {
+__device__ __forceinline__ uint32_t column_pair(const uint32_t* x, const uint32_t* y, int e, const PairScale& p, const Biases& bs) {
   if constexpr (BITS == 16) {
-    return GEAR_BYTE_PERM(b[e >> 1], a[e >> 1], (e & 1) ? 0x07060302u : 0x05040100u);
+    return GEAR_BYTE_PERM(y[e >> 1], x[e >> 1], (e & 1) ? 0x07060302u : 0x05040100u);
   } else if constexpr (BITS == 8) {
-    const uint32_t x = a[e >> 2], y = b[e >> 2];
-    const int k = e & 3;
-    if constexpr (BF) return value_bf16((x >> (8 * k)) & 0xFFu, (y >> (8 * k)) & 0xFFu, p);
-    else return value_f16(GEAR_BYTE_PERM(y, x, 0x0C040C00u + 0x00010001u * (uint32_t)k) | F16_1024, F16_NEG_1024, p);
+    const uint32_t w = (e & 2) ? y[e >> 2] : x[e >> 2];
+    if constexpr (BF) return value_bf16((w >> (16 * (e & 1))) & 0xFFu, (w >> (16 * (e & 1) + 8)) & 0xFFu, p);
+    else return value_f16(GEAR_BYTE_PERM(BYTES_64H, w, (e & 1) ? 0x04030402u : 0x04010400u), F16_NEG_1024, p);
   } else {
-    const uint32_t w = (e & 1) ? b[0] : a[0];
-    const int i = e >> 1;
-    if constexpr (BF) {
-      return value_bf16((w >> (4 * i)) & 0xFu, (w >> (4 * i + 16)) & 0xFu, p);
-    } else {
-      const uint32_t x = i < 2 ? w : w >> 8;
-      return (i & 1) ? value_f16((x & 0x00F000F0u) | F16_64, F16_NEG_64, p) : value_f16((x & 0x000F000Fu) | F16_1024, F16_NEG_1024, p);
-    }
+    return row_pair<4, BF>((e & 1) ? y[0] : x[0], 0u, e >> 1, p, bs);   // (nibble e / 2 of each half)
   }
 }
 
@@ -182,19 +200,21 @@ struct PageAttn {
   int32_t width;     // entries of a sequence's row of the table
   int32_t n_seqs, n_tokens, gq, causal;
   int32_t n_split;   // parts of the key axis, at most
+  int32_t least;     // tokens that make a part
   int32_t few;       // columns (new tokens x gq) up to which page_attn_few_kernel has a sequence; 0: page_attn_many_kernel has them all
   int32_t few_cols;  // record rows per sequence and head there
   int32_t tiles;     // column tiles of page_attn_many_kernel, at most
 };
 constexpr int KEY_STEP = 32, MANY_COLS = 128, MANY_KEYS = 64;
-constexpr int FEW_PART = 256, MANY_PART = 512;   // tokens of a part, at least
+constexpr int FEW_PART = 512, MANY_PART = 512;   // tokens of a part, at least
 
-// The key axis of `keys` tokens in at most n_split parts of `unit` x some: tokens of a part, and how many there are (at least one).
+// The key axis of `keys` tokens in at most n_split equal parts of about `least` tokens and more, multiples of `unit`: tokens of a part, and how many
+// there are (at least one).
 struct Parts {
   int len, count;
 };
 __host__ __device__ inline Parts parts_of(int keys, int n_split, int least, int unit) {
-  int n = keys / least;
+  int n = (keys + least / 2) / least;
   n = n < 1 ? 1 : (n > n_split ? n_split : n);
   const int len = ((keys + n - 1) / n + unit - 1) / unit * unit;
   return Parts{len, len > 0 ? (keys + len - 1) / len : 1};

@@ -349,7 +349,7 @@ inline void launch(const void* kernel, const char* name, dim3 grid, dim3 block, 
 #define __builtin_amdgcn_mfma_f32_4x4x1f32(a, b, c, x, y, z) \
   __builtin_bit_cast(gear::floatx4, simt::mfma4x4x1((a), (b), __builtin_bit_cast(simt::f4, (c))))
 #define GEAR_NO_BF16_TYPE
-#define GEAR_SCHED_MFMA_VALU(n) ((void)0)
+#define GEAR_IN_VGPR(x) ((void)0)
 #define GEAR_MFMA16_F16(a, b, c) simt::mfma_n<16>((a), (b), (c), false)
 #define GEAR_MFMA16_BF16(a, b, c) simt::mfma_n<16>((a), (b), (c), true)
 #define GEAR_MFMA32_F16(a, b, c) simt::mfma_n<32>((a), (b), (c), false)

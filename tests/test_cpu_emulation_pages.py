@@ -64,7 +64,7 @@ CASES = [
     Case("few_bf16", BF16, 16, 128, 64, 1, 5, [(6, 90)]),
     Case("few_bf16_8_two_tiles", BF16, 8, 32, 16, 1, 8, [(4, 70), (1, 130)], bad=True),
     Case("few_bf16_4", BF16, 4, 128, 16, 1, 3, [(2, 50)], causal=False),
-    Case("few_split", F16, 8, 128, 16, 1, 2, [(1, 800), (1, 30), (1, 513)], max_kv=800),
+    Case("few_split", F16, 8, 128, 16, 1, 2, [(1, 1100), (1, 30)], max_kv=1100),
     Case("empty_rows", F16, 16, 128, 16, 1, 2, [(9, 4), (1, 0)]),
     Case("many_f16", F16, 16, 128, 16, 1, 2, [(40, 140), (33, 33)], bad=True),
     Case("many_8", F16, 8, 32, 16, 1, 1, [(150, 150)], pad=3),
