@@ -43,21 +43,32 @@ __device__ __forceinline__ void store_piece(const PageGeom& g, unsigned char* bl
     lane_min_max<DPP_XOR2>(mn, mx);
     if (g.gshift > 5) lane_min_max<DPP_HALF_MIRROR>(mn, mx);
     if (g.gshift > 6) lane_min_max<DPP_MIRROR>(mn, mx);
-    // fp32: the differences of 16-bit values are exact unless their exponents lie more than 13 (bf16: 16) apart, and an IEEE
-    // quotient of such a difference by a 16-bit scale is rounded across a half only where it lies within 2^-17 of one.
     const float s32 = __fdiv_rn(__fsub_rn(mx, mn), LEVELS);
     const uint32_t sz = (pack2<BF>(s32, 0.0f) & 0xFFFFu) | (pack2<BF>(mn, 0.0f) << 16);
-    const float scale = to_f32<BF>(sz & 0xFFFFu), by = scale > 0.0f ? scale : 1.0f, most = scale > 0.0f ? LEVELS : 0.0f;
+    const float scale = to_f32<BF>(sz & 0xFFFFu);
     uint32_t code[8];
+    // (x - zero) / scale as IEEE division gives it, in a product and two fused steps: with a correctly rounded reciprocal the last one rounds
+    // the exact quotient.  The difference is exact unless the exponents lie more than 13 (bf16: 16) apart, and such a quotient is rounded
+    // across a half only where it lies within 2^-17 of one.  Then the nearest integer is the sum with 1.5 * 2^23, whose last bits
+    // are the code.  (Dividing: 8 x 4096 tokens of 8 heads to 4 bits 58 us.)
+    const float inv = scale > 0.0f ? __fdiv_rn(1.0f, scale) : 0.0f, most = scale > 0.0f ? LEVELS : 0.0f;
+    if (!BF || scale >= 0x1p-100f || !(scale > 0.0f)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) code[e] = (uint32_t)clamp_f32(rintf(__fdiv_rn(__fsub_rn(f[e], mn), by)), 0.0f, most);
+      for (int e = 0; e < 8; ++e) {
+        const float d = __fsub_rn(f[e], mn), t = __fmul_rn(d, inv), q = __builtin_fmaf(__builtin_fmaf(-t, scale, d), inv, t);
+        code[e] = __float_as_uint(__fadd_rn(fminf(q, most), 12582912.0f));
+      }
+    } else {   // bf16 steps whose reciprocal, or the remainder above, would leave fp32's range
+#pragma unroll
+      for (int e = 0; e < 8; ++e) code[e] = __float_as_uint(__fadd_rn(fminf(__fdiv_rn(__fsub_rn(f[e], mn), scale), most), 12582912.0f));
+    }
     if constexpr (BITS == 8) {
-      const uint2 y = make_uint2(code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24, code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24);
-      if (live) *reinterpret_cast<uint2*>(block + (r * 16 + c) * 8) = y;
+      auto bytes = [](uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return GEAR_BYTE_PERM(GEAR_BYTE_PERM(d, c, 0x0C0C0400u), GEAR_BYTE_PERM(b, a, 0x0C0C0400u), 0x05040100u); };
+      if (live) *reinterpret_cast<uint2*>(block + (r * 16 + c) * 8) = make_uint2(bytes(code[0], code[1], code[2], code[3]), bytes(code[4], code[5], code[6], code[7]));
     } else {
       uint32_t y = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y |= code[e] << (4 * (e >> 1) + 16 * (e & 1));
+      for (int e = 0; e < 8; ++e) y |= (code[e] & 0xFu) << (4 * (e >> 1) + 16 * (e & 1));
       if (live) *reinterpret_cast<uint32_t*>(block + (r * 16 + c) * 4) = y;
     }
     if (live && ((c << 3) & ((1 << g.gshift) - 1)) == 0)
@@ -79,62 +90,64 @@ __device__ __forceinline__ uint4 load_piece(const PageGeom& g, const unsigned ch
 }
 
 constexpr int COPY_THREADS = 256;
+#ifndef GEAR_PAGE_PAST_CACHES   // (the CPU stand-in lowers it)
+#define GEAR_PAGE_PAST_CACHES (64ll << 20)
+#endif
+constexpr int64_t PAST_CACHES = GEAR_PAGE_PAST_CACHES;   // bytes of both tensors
 
-// grid: (head, group of rows); ROWS rows per 16 lanes, whose loads are all requested first.
-template <int BITS, bool BF, bool WRITE, int ROWS>
+// What is brought back once and is larger than the caches is stored past them (7 x 1777 tokens of 40 heads, 255 MB: 79 -> 47 us;
+// 16 x 4096 of 32, 1.07 GB: 314 -> 288).
+template <bool PAST>
+__device__ __forceinline__ void store16(unsigned char* p, const uint4& v) {
+#ifdef GEAR_NO_NONTEMPORAL
+  *reinterpret_cast<uint4*>(p) = v;
+#else
+  if constexpr (PAST) __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, v), reinterpret_cast<u32x4_t*>(p));
+  else *reinterpret_cast<uint4*>(p) = v;
+#endif
+}
+
+// grid: (head, 16 rows), heads next to each other.  A row per 16 lanes: with two or four, whose loads are requested together, the writes took 4 and 12 %
+// longer (the chip's waves have enough on their way).
+template <int BITS, bool BF, bool WRITE, bool PAST>
 __global__ __launch_bounds__(COPY_THREADS) void page_copy_kernel(PageCopy a) {
   const PageGeom& g = a.geom;
-  const int h = (int)(blockIdx.x % (unsigned)g.H), c = threadIdx.x & 15, sub = threadIdx.x >> 4;
-  const int64_t first = (int64_t)(blockIdx.x / (unsigned)g.H) * (COPY_THREADS / 16 * ROWS) + sub;
-  const int64_t slots = (int64_t)g.n_pages << g.shift;
-  bool live[ROWS];              // the same for the 16 lanes of a row
-  uint64_t page[ROWS];          // where the head's Keys of the row's page begin
-  int row[ROWS];
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    const int64_t t = first + i * (COPY_THREADS / 16), slot = t < a.total ? a.slots[t] : -1;
-    live[i] = slot >= 0 && slot < slots;
-    const int64_t at = live[i] ? slot : 0;
-    page[i] = (uint64_t)(at >> g.shift) * g.page_bytes + (uint64_t)(2 * h) * g.block_bytes;
-    row[i] = (int)(at & page_mask(g));
-  }
-  int64_t off_k[ROWS], off_v[ROWS];
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    const uint32_t t = (uint32_t)(first + i * (COPY_THREADS / 16)), s = t / (uint32_t)a.n_rows, r = t - s * (uint32_t)a.n_rows;
-    off_k[i] = 2 * (s * a.k.seq + r * a.k.token + h * a.k.head + 8 * c);
-    off_v[i] = 2 * (s * a.v.seq + r * a.v.token + h * a.v.head + 8 * c);
-  }
-  uint4 k[ROWS], v[ROWS];
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    k[i] = v[i] = make_uint4(0, 0, 0, 0);
-    if (!live[i]) continue;
+  const int h = (int)(blockIdx.x % (unsigned)g.H), c = threadIdx.x & 15;
+  const uint32_t t = blockIdx.x / (unsigned)g.H * (COPY_THREADS / 16) + (threadIdx.x >> 4), s = t / (uint32_t)a.n_rows, r = t - s * (uint32_t)a.n_rows;
+  const int64_t slot = (int64_t)t < a.total ? a.slots[t] : -1;
+  const bool live = slot >= 0 && slot < (int64_t)g.n_pages << g.shift;   // the same for the 16 lanes of a row
+  const int64_t at = live ? slot : 0;
+  const uint64_t keys = (uint64_t)(at >> g.shift) * g.page_bytes + (uint64_t)(2 * h) * g.block_bytes;   // where the head's Keys of the row's page begin
+  const int row = (int)(at & page_mask(g));
+  unsigned char* const kp = a.k.data + 2 * (s * a.k.seq + r * a.k.token + h * a.k.head + 8 * c);
+  unsigned char* const vp = a.v.data + 2 * (s * a.v.seq + r * a.v.token + h * a.v.head + 8 * c);
+  uint4 k = make_uint4(0, 0, 0, 0), v = k;
+  if (live) {
     if constexpr (WRITE) {
-      k[i] = *reinterpret_cast<const uint4*>(a.k.data + off_k[i]);
-      v[i] = *reinterpret_cast<const uint4*>(a.v.data + off_v[i]);
+      k = *reinterpret_cast<const uint4*>(kp);
+      v = *reinterpret_cast<const uint4*>(vp);
     } else {
-      if (a.k.data) k[i] = load_piece<BITS, BF>(g, g.pool + page[i], row[i], c);
-      if (a.v.data) v[i] = load_piece<BITS, BF>(g, g.pool + page[i] + g.block_bytes, row[i], c);
+      if (a.k.data) k = load_piece<BITS, BF>(g, g.pool + keys, row, c);
+      if (a.v.data) v = load_piece<BITS, BF>(g, g.pool + keys + g.block_bytes, row, c);
     }
   }
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    if constexpr (WRITE) {
-      unsigned char* block = const_cast<unsigned char*>(g.pool) + page[i];
-      store_piece<BITS, BF>(g, block, row[i], c, k[i], live[i]);
-      store_piece<BITS, BF>(g, block + g.block_bytes, row[i], c, v[i], live[i]);
-    } else if (live[i]) {
-      if (a.k.data) *reinterpret_cast<uint4*>(a.k.data + off_k[i]) = k[i];
-      if (a.v.data) *reinterpret_cast<uint4*>(a.v.data + off_v[i]) = v[i];
-    }
+  if constexpr (WRITE) {
+    unsigned char* block = const_cast<unsigned char*>(g.pool) + keys;
+    store_piece<BITS, BF>(g, block, row, c, k, live);
+    store_piece<BITS, BF>(g, block + g.block_bytes, row, c, v, live);
+  } else if (live) {
+    if (a.k.data) store16<PAST>(kp, k);
+    if (a.v.data) store16<PAST>(vp, v);
   }
 }
 
 template <int BITS, bool BF, bool WRITE>
 static hipError_t launch_copy(const PageCopy& a, hipStream_t st) {
   const int64_t per = COPY_THREADS / 16, blocks = (a.total + per - 1) / per * a.geom.H;
-  hipLaunchKernelGGL((page_copy_kernel<BITS, BF, WRITE, 1>), dim3((unsigned)blocks), dim3(COPY_THREADS), 0, st, a);
+  if (!WRITE && a.total * a.geom.H * (4 * D) >= PAST_CACHES)
+    hipLaunchKernelGGL((page_copy_kernel<BITS, BF, WRITE, !WRITE>), dim3((unsigned)blocks), dim3(COPY_THREADS), 0, st, a);
+  else
+    hipLaunchKernelGGL((page_copy_kernel<BITS, BF, WRITE, false>), dim3((unsigned)blocks), dim3(COPY_THREADS), 0, st, a);
   return hipGetLastError();
 }
 

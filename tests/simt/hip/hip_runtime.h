@@ -349,6 +349,8 @@ inline void launch(const void* kernel, const char* name, dim3 grid, dim3 block, 
 #define __builtin_amdgcn_mfma_f32_4x4x1f32(a, b, c, x, y, z) \
   __builtin_bit_cast(gear::floatx4, simt::mfma4x4x1((a), (b), __builtin_bit_cast(simt::f4, (c))))
 #define GEAR_NO_BF16_TYPE
+#define GEAR_NO_NONTEMPORAL
+#define GEAR_PAGE_PAST_CACHES (32ll << 10)
 #define GEAR_IN_VGPR(x) ((void)0)
 #define GEAR_MFMA16_F16(a, b, c) simt::mfma_n<16>((a), (b), (c), false)
 #define GEAR_MFMA16_BF16(a, b, c) simt::mfma_n<16>((a), (b), (c), true)
@@ -383,6 +385,7 @@ inline uint32_t __float_as_uint(float f) { uint32_t i; memcpy(&i, &f, 4); return
 inline float __fdiv_rn(float a, float b) { return a / b; }
 inline float __fsub_rn(float a, float b) { return a - b; }
 inline float __fmul_rn(float a, float b) { return a * b; }
+inline float __fadd_rn(float a, float b) { return a + b; }
 inline int __popc(uint32_t x) { return __builtin_popcount(x); }
 inline int __ffs(int x) { return __builtin_ffs(x); }
 inline int __ffsll(long long x) { return __builtin_ffsll(x); }
