@@ -15,10 +15,21 @@ struct PageCopy {
   int64_t total;      // rows of all sequences, below 2^31
 };
 
+typedef short i16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t min_i16x2(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(i16x2_t, a), __builtin_bit_cast(i16x2_t, b)));
+}
+__device__ __forceinline__ uint32_t max_i16x2(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(i16x2_t, a), __builtin_bit_cast(i16x2_t, b)));
+}
+// Two 16-bit floating numbers as signed integers of the same order, and back.
+__device__ __forceinline__ uint32_t ordered(uint32_t x) {
+  return x ^ (__builtin_bit_cast(uint32_t, __builtin_bit_cast(i16x2_t, x) >> 15) & 0x7FFF7FFFu);
+}
 template <int CTRL>
-__device__ __forceinline__ void lane_min_max(float& mn, float& mx) {
-  mn = fminf(mn, dpp_f<CTRL>(mn));
-  mx = fmaxf(mx, dpp_f<CTRL>(mx));
+__device__ __forceinline__ void lane_extremes(uint32_t& lo, uint32_t& hi) {
+  lo = min_i16x2(lo, dpp_u<CTRL>(lo));
+  hi = max_i16x2(hi, dpp_u<CTRL>(hi));
 }
 
 // One row piece of eight values into its place: `block` the head's Keys or Values in the page, r the row, c the lane's piece (0..15).  Every
@@ -33,25 +44,34 @@ __device__ __forceinline__ void store_piece(const PageGeom& g, unsigned char* bl
     float f[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] = to_f32<BF>(w[e >> 1] >> (16 * (e & 1)) & 0xFFFFu);
-    float mn = f[0], mx = f[0];
+    // extremes: two values at a time as signed 16-bit integers of the same order (negative ones with their other bits turned around)
+    uint32_t lo = ordered(w[0]), hi = lo;
 #pragma unroll
-    for (int e = 1; e < 8; ++e) {
-      mn = fminf(mn, f[e]);
-      mx = fmaxf(mx, f[e]);
+    for (int j = 1; j < 4; ++j) {
+      const uint32_t k = ordered(w[j]);
+      lo = min_i16x2(lo, k);
+      hi = max_i16x2(hi, k);
     }
-    lane_min_max<DPP_XOR1>(mn, mx);
-    lane_min_max<DPP_XOR2>(mn, mx);
-    if (g.gshift > 5) lane_min_max<DPP_HALF_MIRROR>(mn, mx);
-    if (g.gshift > 6) lane_min_max<DPP_MIRROR>(mn, mx);
-    const float s32 = __fdiv_rn(__fsub_rn(mx, mn), LEVELS);
-    const uint32_t sz = (pack2<BF>(s32, 0.0f) & 0xFFFFu) | (pack2<BF>(mn, 0.0f) << 16);
+    lane_extremes<DPP_XOR1>(lo, hi);
+    lane_extremes<DPP_XOR2>(lo, hi);
+    if (g.gshift > 5) lane_extremes<DPP_HALF_MIRROR>(lo, hi);
+    if (g.gshift > 6) lane_extremes<DPP_MIRROR>(lo, hi);
+    lo = min_i16x2(lo, lo >> 16 | lo << 16);
+    hi = max_i16x2(hi, hi >> 16 | hi << 16);
+    const uint32_t zero = ordered(lo) & 0xFFFFu;
+    const float mn = to_f32<BF>(zero), mx = to_f32<BF>(ordered(hi) & 0xFFFFu);
+    // (a quotient as below; 1 / 255 and 1 / 15 are constants)
+    const float range = __fsub_rn(mx, mn), by = __fmul_rn(range, 1.0f / LEVELS);
+    float s32 = __builtin_fmaf(__builtin_fmaf(-by, LEVELS, range), 1.0f / LEVELS, by);
+    GEAR_IN_VGPR(s32);   // (rounded here: else the last step and the rounding to fp16 become one instruction, which rounds another number once)
+    const uint32_t sz = (pack2<BF>(s32, 0.0f) & 0xFFFFu) | zero << 16;
     const float scale = to_f32<BF>(sz & 0xFFFFu);
     uint32_t code[8];
     // (x - zero) / scale as IEEE division gives it, in a product and two fused steps: with a correctly rounded reciprocal the last one rounds
     // the exact quotient.  The difference is exact unless the exponents lie more than 13 (bf16: 16) apart, and such a quotient is rounded
     // across a half only where it lies within 2^-17 of one.  Then the nearest integer is the sum with 1.5 * 2^23, whose last bits
     // are the code.  (Dividing: 8 x 4096 tokens of 8 heads to 4 bits 58 us.)
-    const float inv = scale > 0.0f ? __fdiv_rn(1.0f, scale) : 0.0f, most = scale > 0.0f ? LEVELS : 0.0f;
+    const float inv = scale > 0.0f ? recip_of_half(scale) : 0.0f, most = scale > 0.0f ? LEVELS : 0.0f;
     if (!BF || scale >= 0x1p-100f || !(scale > 0.0f)) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
