@@ -15,7 +15,7 @@ CSRC_PAGES = os.path.join(PKG, "csrc_pages")   # the paged cache
 
 SOURCES = [os.path.join(CSRC, s) for s in ("gear_api.hip", "compress_filter.hip", "compress_values.hip", "lowrank.hip", "decode.hip",
                                            "decompress_export.hip")]
-SOURCES += [os.path.join(CSRC_PAGES, s) for s in ("page_api.hip", "page_copy.hip", "page_few.hip", "page_many.hip")]
+SOURCES += [os.path.join(CSRC_PAGES, s) for s in ("page_api.hip", "page_copy.hip", "page_few.hip", "page_many.hip", "page_mixed.hip")]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -58,6 +58,12 @@ PagePlan page_plan(int H, int gq, int n_seqs, int n_tokens, int max_q, int max_k
     p.many_least = max_kv / p.many_split > MANY_PART ? max_kv / p.many_split : MANY_PART;
     if (p.many_split > 1) p.many_rows = (int64_t)n_tokens * H * gq;
   }
+  // Both in one launch (page_mixed.hip), but where the few columns' bytes take most of the time, and long: there their blocks are better off with eight waves
+  // and the chip to themselves.  Estimates in us, at 6 TB/s and 1 PFLOP/s, from the bounds alone.  (One launch and two: 33 sequences of up to 4000 tokens,
+  // three of them chunks of up to 700, 110 and 150 us; 20 of up to 1000 tokens, one chunk of 100, 34 and 50; 10 of up to 5908 tokens of 32
+  // heads at 16 bits, two chunks of 415, 231 and 194.)
+  const double few_us = (double)n_seqs * H * max_kv * bytes_per_key / 6e6, many_us = (double)n_tokens * H * gq * max_kv * 512.0 / 1e9;
+  p.one_launch = p.few && p.many && !(few_us > 100.0 && few_us > 2.0 * many_us);
   return p;
 }
 
@@ -211,7 +217,7 @@ int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_by
     if (workspace_bytes < RECORD_BYTES * (size_t)(few_recs + many_recs)) return GEAR_ECAPACITY;
   }
   const int64_t tiles = (int64_t)b.n_tokens * gq / MANY_COLS + b.n_seqs;
-  if ((int64_t)b.n_seqs * H * p.few_split > INT_MOST || tiles * H * p.many_split > INT_MOST) return GEAR_ECAPACITY;
+  if ((int64_t)b.n_seqs * H * p.few_split + tiles * H * p.many_split > INT_MOST) return GEAR_ECAPACITY;
 
   a.q_start = b.q_start;
   a.kv_len = b.kv_len;
@@ -231,22 +237,18 @@ int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_by
   float* rec = static_cast<float*>(workspace);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   const bool bf = cfg->dtype == GEAR_BF16;
-  if (p.many) {   // the longer kernel first
-    PageAttn m = a;
-    m.n_split = p.many_split;
-    m.least = p.many_least;
-    m.rec_o = rec;
-    m.rec_ml = reinterpret_cast<float2*>(rec + many_recs * D);
-    if (launch_page_many(m, cfg->bits, bf, st) != hipSuccess) return GEAR_EHIP;
-  }
-  if (p.few) {
-    PageAttn f = a;
-    f.n_split = p.few_split;
-    f.least = FEW_PART;
-    f.rec_o = rec + many_recs * (D + 2);
-    f.rec_ml = reinterpret_cast<float2*>(f.rec_o + few_recs * D);
-    if (launch_page_few(f, cfg->bits, bf, p.few_tiles, st) != hipSuccess) return GEAR_EHIP;
-  }
+  PageAttn m = a, f = a;
+  m.n_split = p.many_split;
+  m.least = p.many_least;
+  m.rec_o = rec;
+  m.rec_ml = reinterpret_cast<float2*>(rec + many_recs * D);
+  f.n_split = p.few_split;
+  f.least = FEW_PART;
+  f.rec_o = rec + many_recs * (D + 2);
+  f.rec_ml = reinterpret_cast<float2*>(f.rec_o + few_recs * D);
+  if (p.one_launch) return launch_page_mixed(m, f, cfg->bits, bf, p.few_tiles, st) == hipSuccess ? GEAR_OK : GEAR_EHIP;
+  if (p.many && launch_page_many(m, cfg->bits, bf, st) != hipSuccess) return GEAR_EHIP;
+  if (p.few && launch_page_few(f, cfg->bits, bf, p.few_tiles, st) != hipSuccess) return GEAR_EHIP;
   return GEAR_OK;
 }
 

@@ -1,328 +1,22 @@
-// Attention of few query columns over pages: single tokens, speculative rows, the tail of a chunk.
-//
-// A sequence's columns are its (new token, query head of the KV head) pairs; up to 16 or 32 of them share one pass over the
-// keys.  A wave takes 32 keys at a time, and works on them without LDS: S^T = K Q^T with the keys as the rows of the 16x16x32
-// instruction, straight from 16-byte loads; a lane of the result then holds, for its column, eight keys (four of each 16) --
-// exactly the eight that the B operand of O^T = V^T P^T wants from it, if the contraction runs over the keys in that order.  The
-// A operand of that product needs, for a channel, the same eight keys: the lane loads eight channels (16 c / b bytes) of its
-// eight rows and pairs rows by byte permutations, one per two values, so that product t of eight has channel 8 (l % 16) + t
-// in row l % 16, and the lane's results are 32 consecutive channels of its column.
-//
-// Bound by the pages' bytes; the conversions of 8 and 4 bit codes take a fifth and two fifths of the vector units beside them.
-// The keys are divided among the waves of a block and, where the sequences and heads are few, among blocks, whose records
-// page_merge_kernel joins.
+// Attention of few query columns over pages (page_few.h): the launch, and the joining of the parts.
+#include "page_few.h"
 #include "page_launch.h"
 
 namespace gear {
 
+// Eight waves: with four, and twice the blocks, one token behind 32768 took 21 us instead of 18, two tiles of columns 196 instead of 173 in a mixed batch.
 constexpr int FEW_WAVES = 8;
-
-// 16 keys' rows of one head as loaded.
-template <int BITS>
-struct KeyRows {
-  static constexpr int LOADS = BITS / 4;         // 16-byte pieces of a lane's share of a row (32 channels)
-  uint4 w[LOADS];
-  uint32_t sz[BITS == 8 ? 2 : 1];
-};
-// ... the A operand of product t (0..3): channels first_channel(t, l / 16) + 0..7 of key l % 16
-template <int BITS>
-__device__ __forceinline__ int first_channel(int t, int hh) {
-  constexpr int PIECE = 128 / BITS;              // channels of a 16-byte piece: 8, 16, 32
-  constexpr int PER = PIECE / 8;                 // products per piece
-  return (t / PER) * 4 * PIECE + hh * PIECE + (t % PER) * 8;
-}
-// A lane's places in 16 rows: Keys of row c = l % 16, Values of rows 4 hh + 0..3, hh = l / 16; relative to the first row and its words.
-template <int BITS>
-struct LaneOffsets {
-  uint32_t key, value, key_word[BITS == 8 ? 2 : 1], value_word;
-};
-template <int BITS>
-__device__ __forceinline__ LaneOffsets<BITS> lane_offsets(const PageGeom& g, int c, int hh) {
-  LaneOffsets<BITS> o{};
-  o.key = c * (16 * BITS) + hh * 16;
-  o.value = 4 * hh * (16 * BITS) + c * BITS;
-  if constexpr (BITS < 16) {
-#pragma unroll
-    for (int u = 0; u < KeyRows<BITS>::LOADS; ++u) o.key_word[u] = 4 * (((uint32_t)(first_channel<BITS>(u * (16 / BITS), hh) >> g.gshift) << g.shift) + c);
-    o.value_word = 4 * (((uint32_t)((8 * c) >> g.gshift) << g.shift) + 4 * hh);
-  }
-  return o;
-}
-template <int BITS>
-__device__ __forceinline__ void load_keys(KeyRows<BITS>& k, const PageGeom& g, const unsigned char* block, uint32_t row0, const LaneOffsets<BITS>& o) {
-  const auto rows = GEAR_BUF_MAKE(block + row0 * (16 * BITS), 16 * (16 * BITS));
-#pragma unroll
-  for (int u = 0; u < KeyRows<BITS>::LOADS; ++u) k.w[u] = GEAR_BUF_LOAD16(rows, o.key + 64 * u);
-  if constexpr (BITS < 16) {
-    const auto words = GEAR_BUF_MAKE(block + words_at(g) + row0 * 4, g.block_bytes - words_at(g) - row0 * 4);
-#pragma unroll
-    for (int u = 0; u < KeyRows<BITS>::LOADS; ++u) k.sz[u] = GEAR_BUF_LOAD4(words, o.key_word[u]);
-  }
-}
-template <int BITS, bool BF>
-__device__ __forceinline__ uint4 key_operand(const KeyRows<BITS>& k, int t, const Biases& bs) {
-  if constexpr (BITS == 16) {
-    return k.w[t];
-  } else if constexpr (BITS == 8) {
-    const uint4& w = k.w[t >> 1];
-    const PairScale p = pair_scale<BF>(k.sz[t >> 1], k.sz[t >> 1]);
-    return (t & 1) ? row_run<8, BF>(w.z, w.w, p, bs) : row_run<8, BF>(w.x, w.y, p, bs);
-  } else {
-    const uint4& w = k.w[0];
-    const PairScale p = pair_scale<BF>(k.sz[0], k.sz[0]);
-    return row_run<4, BF>(t == 0 ? w.x : t == 1 ? w.y : t == 2 ? w.z : w.w, 0u, p, bs);
-  }
-}
-// Eight channels of four consecutive rows.
-template <int BITS>
-struct ValueRows {
-  static constexpr int WORDS = BITS / 4;         // 32-bit words of eight channels: 4, 2, 1
-  uint32_t w[4][WORDS];
-  uint32_t sz[4];
-};
-template <int BITS>
-__device__ __forceinline__ void load_values(ValueRows<BITS>& v, const PageGeom& g, const unsigned char* block, uint32_t row0, const LaneOffsets<BITS>& o) {
-  const auto rows = GEAR_BUF_MAKE(block + row0 * (16 * BITS), 16 * (16 * BITS));
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (BITS == 16) {
-      const uint4 x = GEAR_BUF_LOAD16(rows, o.value + i * 256);
-      v.w[i][0] = x.x;
-      v.w[i][1] = x.y;
-      v.w[i][2] = x.z;
-      v.w[i][3] = x.w;
-    } else if constexpr (BITS == 8) {
-      const uint2 x = GEAR_BUF_LOAD8(rows, o.value + i * 128);
-      v.w[i][0] = x.x;
-      v.w[i][1] = x.y;
-    } else {
-      v.w[i][0] = GEAR_BUF_LOAD4(rows, o.value + i * 64);
-    }
-  }
-  if constexpr (BITS < 16) {   // (four rows of a page of 16 and more: 16-byte aligned)
-    const auto words = GEAR_BUF_MAKE(block + words_at(g) + row0 * 4, g.block_bytes - words_at(g) - row0 * 4);
-    const uint4 x = GEAR_BUF_LOAD16(words, o.value_word);
-    v.sz[0] = x.x;
-    v.sz[1] = x.y;
-    v.sz[2] = x.z;
-    v.sz[3] = x.w;
-  }
-}
-template <int BITS>
-__device__ __forceinline__ void drop_value(ValueRows<BITS>& v, int i) {   // a row that no column sees: whatever lies there, 0
-#pragma unroll
-  for (int j = 0; j < ValueRows<BITS>::WORDS; ++j) v.w[i][j] = 0u;
-  v.sz[i] = 0u;
-}
-template <int BITS>
-struct KeyBlock {   // 32 keys
-  KeyRows<BITS> k[2];
-  ValueRows<BITS> v[2];
-};
 
 template <int BITS, bool BF, int NC>
 __global__ __launch_bounds__(64 * FEW_WAVES) void page_attn_few_kernel(PageAttn a) {
-  GEAR_DYN_LDS(lds);   // the block's states: [wave][column] maxima and sums, [wave][NC][8][lane] partial sums
-  const PageGeom& g = a.geom;
-  const int bid = (int)blockIdx.x, head = bid % g.H, rest = bid / g.H, part = rest % a.n_split, s = rest / a.n_split;
-  const int lane = lane_id(), wave = GEAR_WAVE_UNIFORM((int)(threadIdx.x >> 6)), c = lane & 15, hh = lane >> 4;
-  const SeqSpan sp = seq_span(a, s);
-  const int cols = sp.nq * a.gq;
-  if (sp.nq <= 0 || sp.nq > a.few || cols > a.few) return;
-  const Parts parts = parts_of(sp.kv, a.n_split, a.least, KEY_STEP);
-  if (part >= parts.count) return;
-  const int k0 = part * parts.len, k1 = min(sp.kv, k0 + parts.len);
-
-  // the columns' query rows, as B operands; what they see
-  uint4 q[NC][4];
-  int sees[NC];
-#pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    const int col = n * 16 + c, row = col / a.gq, j = col - row * a.gq;
-    sees[n] = 0;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) q[n][t] = make_uint4(0, 0, 0, 0);
-    if (col < cols) {
-      sees[n] = row_sees(a, sp, row);
-      const unsigned char* p = a.q.data + 2 * ((int64_t)(sp.q0 + row) * a.q.token + (int64_t)(head * a.gq + j) * a.q.head);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) q[n][t] = signed_query(*reinterpret_cast<const uint4*>(p + 2 * first_channel<BITS>(t, hh)), a.flip);
-    }
-  }
-  const int all_see = row_sees(a, sp, 0);   // every column sees the keys before this one
-
-  floatx4 o[NC][8];
-  float m[NC], l[NC];
-#pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    m[n] = -INFINITY;
-    l[n] = 0.0f;
-#pragma unroll
-    for (int t = 0; t < 8; ++t) o[n][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
-  PageRow pages = page_row(a, s, k1);
-  const Biases bs = biases();
-  const LaneOffsets<BITS> offsets = lane_offsets<BITS>(g, c, hh);
-  auto fetch = [&](KeyBlock<BITS>& x, int key, int p0, int p1) {   // (a key without a page reads page 0, and counts for nothing)
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int p = b == 0 ? p0 : p1;
-      const unsigned char* block = g.pool + (uint64_t)(p < 0 ? 0 : p) * g.page_bytes + (uint64_t)(2 * head) * g.block_bytes;
-      const uint32_t row0 = (uint32_t)(key + 16 * b) & page_mask(g);
-      load_keys<BITS>(x.k[b], g, block, row0, offsets);
-      load_values<BITS>(x.v[b], g, block + g.block_bytes, row0, offsets);
-    }
-  };
-  const int stride = KEY_STEP * FEW_WAVES;
-  for (int key = k0 + KEY_STEP * wave; key < k1; key += stride) {
-    const int p0 = page_of(pages, key), p1 = page_of(pages, key + 16);
-    KeyBlock<BITS> x;
-    fetch(x, key, p0, p1);
-    // scores: keys 4 hh + 0..3 of each 16, column c
-    floatx4 score[NC][2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-#pragma unroll
-      for (int n = 0; n < NC; ++n) score[n][b] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const uint4 ka = key_operand<BITS, BF>(x.k[b], t, bs);
-#pragma unroll
-        for (int n = 0; n < NC; ++n) score[n][b] = mfma16<BF>(ka, q[n][t], score[n][b]);
-      }
-    }
-    const bool edge = key + KEY_STEP > all_see || p0 < 0 || p1 < 0;   // some column does not see some of the keys
-    if (edge) {
-      int first = key + 4 * hh;
-      GEAR_PIN_VGPR(first);   // (what depends on it stays in here: as selections on `edge` every step would pay for it)
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int at = first + 16 * b + i;
-          const bool there = (b == 0 ? p0 : p1) >= 0;
-          if (!there || at >= sp.kv) drop_value<BITS>(x.v[b], i);
-#pragma unroll
-          for (int n = 0; n < NC; ++n)
-            if (!there || at >= sees[n]) score[n][b][i] = -INFINITY;
-        }
-    }
-    uint4 pw[NC];
-#pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      float top = -INFINITY;
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          top = fmaxf(top, score[n][b][i]);
-        }
-      top = col_max<true>(top) * a.scale_log2;
-      if (__ballot(top > m[n]) != 0ull) {
-        const float now = fmaxf(m[n], top), by = now == -INFINITY ? 1.0f : GEAR_EXP2(m[n] - now);
-        m[n] = now;
-        l[n] *= by;
-#pragma unroll
-        for (int t = 0; t < 8; ++t) o[n][t] *= by;
-      }
-      const float from = m[n] == -INFINITY ? 0.0f : m[n];
-      float p[8];
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[4 * b + i] = GEAR_EXP2(__builtin_fmaf(score[n][b][i], a.scale_log2, -from));
-          l[n] += p[4 * b + i];
-        }
-      // rounded to the type for the product (2^-11 or 2^-8 of each weight, as the outputs are); the sum keeps them in fp32
-      pw[n] = make_uint4(pack2<BF>(p[0], p[1]), pack2<BF>(p[2], p[3]), pack2<BF>(p[4], p[5]), pack2<BF>(p[6], p[7]));
-    }
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      column_words<BITS>(x.v[b].w[0], x.v[b].w[1]);
-      column_words<BITS>(x.v[b].w[2], x.v[b].w[3]);
-    }
-    PairScale ps[4];
-    if constexpr (BITS < 16) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        ps[2 * b] = pair_scale<BF>(x.v[b].sz[0], x.v[b].sz[1]);
-        ps[2 * b + 1] = pair_scale<BF>(x.v[b].sz[2], x.v[b].sz[3]);
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      uint32_t w[4];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        w[2 * b] = column_pair<BITS, BF>(x.v[b].w[0], x.v[b].w[1], t, ps[2 * b], bs);
-        w[2 * b + 1] = column_pair<BITS, BF>(x.v[b].w[2], x.v[b].w[3], t, ps[2 * b + 1], bs);
-      }
-      const uint4 va = make_uint4(w[0], w[1], w[2], w[3]);
-#pragma unroll
-      for (int n = 0; n < NC; ++n) o[n][t] = mfma16<BF>(va, pw[n], o[n][t]);
-    }
-  }
-
-  // the waves' states: every wave brings its own to the common maximum, then sums and stores a share of the channels
-  constexpr int waves = FEW_WAVES;
-  float* top_of = reinterpret_cast<float*>(lds);                   // [wave][NC * 16]
-  float* sum_of = top_of + waves * NC * 16;
-  float4* part_of = reinterpret_cast<float4*>(sum_of + waves * NC * 16);
-#pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    l[n] = col_sum<true>(l[n]);
-    if (hh == 0) {
-      top_of[wave * NC * 16 + n * 16 + c] = m[n];
-      sum_of[wave * NC * 16 + n * 16 + c] = l[n];
-    }
-  }
-  block_lds_sync();
-  float total[NC], top[NC];
-#pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    top[n] = -INFINITY;
-    for (int w = 0; w < waves; ++w) top[n] = fmaxf(top[n], top_of[w * NC * 16 + n * 16 + c]);
-    const float from = top[n] == -INFINITY ? 0.0f : top[n];
-    total[n] = 0.0f;
-    for (int w = 0; w < waves; ++w) total[n] += sum_of[w * NC * 16 + n * 16 + c] * GEAR_EXP2(top_of[w * NC * 16 + n * 16 + c] - from);
-    const float by = GEAR_EXP2(m[n] - from);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {   // channels 32 hh + 8 i + 0..7
-      part_of[((wave * NC + n) * 8 + 2 * i) * 64 + lane] = make_float4(o[n][0][i] * by, o[n][1][i] * by, o[n][2][i] * by, o[n][3][i] * by);
-      part_of[((wave * NC + n) * 8 + 2 * i + 1) * 64 + lane] = make_float4(o[n][4][i] * by, o[n][5][i] * by, o[n][6][i] * by, o[n][7][i] * by);
-    }
-  }
-  block_lds_sync();
-  for (int piece = wave; piece < NC * 8; piece += waves) {
-    const int n = piece >> 3, k = piece & 7, col = n * 16 + c;
-    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int w = 0; w < waves; ++w) {
-      const float4 y = part_of[((w * NC + n) * 8 + k) * 64 + lane];
-      x.x += y.x;
-      x.y += y.y;
-      x.z += y.z;
-      x.w += y.w;
-    }
-    if (col >= cols) continue;
-    const float sum = NC == 1 || n == 0 ? total[0] : total[NC - 1];
-    const int ch = 32 * hh + 4 * k;
-    if (parts.count == 1) {
-      const float r = sum > 0.0f ? 1.0f / sum : 0.0f;
-      const int row = col / a.gq, j = col - row * a.gq;
-      unsigned char* p = a.out.data + 2 * ((int64_t)(sp.q0 + row) * a.out.token + (int64_t)(head * a.gq + j) * a.out.head + ch);
-      *reinterpret_cast<uint2*>(p) = make_uint2(pack2<BF>(x.x * r, x.y * r), pack2<BF>(x.z * r, x.w * r));
-    } else {
-      const int64_t rec = (((int64_t)s * g.H + head) * a.few_cols + col) * a.n_split + part;
-      *reinterpret_cast<float4*>(a.rec_o + rec * D + ch) = x;
-      if (ch == 0) a.rec_ml[rec] = make_float2(NC == 1 || n == 0 ? top[0] : top[NC - 1], sum);
-    }
-  }
+  GEAR_DYN_LDS(lds);
+  few_columns<BITS, BF, NC, FEW_WAVES>(a, (int)blockIdx.x, lds);
 }
 
-// The records of a column's parts become its output: the weight of a part is 2^(its maximum - the greatest) .  One block of four
-// waves per column, a wave per four parts; a lane has two channels.
-__global__ __launch_bounds__(64 * FEW_WAVES) void page_merge_few_kernel(PageAttn a, int bf) {
+// The records of a column's parts become its output: the weight of a part is 2^(its maximum - the greatest).  One block of four waves per
+// column; a lane has two channels.
+constexpr int MERGE_WAVES = 4;
+__global__ __launch_bounds__(64 * MERGE_WAVES) void page_merge_few_kernel(PageAttn a, int bf) {
   GEAR_DYN_LDS(lds);
   const PageGeom& g = a.geom;
   const int bid = (int)blockIdx.x, col = bid % a.few_cols, rest = bid / a.few_cols, head = rest % g.H, s = rest / g.H;
@@ -331,24 +25,29 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_merge_few_kernel(PageAttn
   if (sp.nq <= 0 || sp.nq > a.few || cols > a.few || col >= cols) return;
   const Parts parts = parts_of(sp.kv, a.n_split, a.least, KEY_STEP);
   if (parts.count <= 1) return;
-  const int lane = lane_id(), wave = (int)(threadIdx.x >> 6);
+  const int lane = lane_id(), wave = (int)(threadIdx.x >> 6), count = parts.count;
   const int64_t rec = (((int64_t)s * g.H + head) * a.few_cols + col) * a.n_split;
-  float top = -INFINITY;
-  for (int i = lane; i < parts.count; i += 64) top = fmaxf(top, a.rec_ml[rec + i].x);
-  top = wave_max(top);
-  const float from = top == -INFINITY ? 0.0f : top;
-  float sum = 0.0f, x = 0.0f, y = 0.0f;
-  for (int i0 = wave; i0 < parts.count; i0 += FEW_WAVES * 8) {   // eight records on their way at a time
-    float2 ml[8], v[8];
+  // A wave's records on their way, eight at a time, with the first maxima; every wave finds the greatest of all.
+  float2 ml[8], v[8];
+  auto request = [&](int i0) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const int64_t i = rec + min(i0 + FEW_WAVES * u, parts.count - 1);
+      const int64_t i = rec + min(i0 + MERGE_WAVES * u, count - 1);
       ml[u] = a.rec_ml[i];
       v[u] = *reinterpret_cast<const float2*>(a.rec_o + i * D + 2 * lane);
     }
+  };
+  request(wave);
+  float top = a.rec_ml[rec + min(lane, count - 1)].x;
+  for (int i = lane + 64; i < count; i += 64) top = fmaxf(top, a.rec_ml[rec + i].x);
+  top = wave_max(top);
+  const float from = top == -INFINITY ? 0.0f : top;
+  float sum = 0.0f, x = 0.0f, y = 0.0f;
+  for (int i0 = wave; i0 < count; i0 += MERGE_WAVES * 8) {
+    if (i0 != wave) request(i0);
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const float by = i0 + FEW_WAVES * u < parts.count ? GEAR_EXP2(ml[u].x - from) : 0.0f;
+      const float by = i0 + MERGE_WAVES * u < count ? GEAR_EXP2(ml[u].x - from) : 0.0f;
       sum += ml[u].y * by;
       x += v[u].x * by;
       y += v[u].y * by;
@@ -360,7 +59,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_merge_few_kernel(PageAttn
   sh[(wave * 3 + 2) * 64 + lane] = y;
   block_lds_sync();
   if (wave != 0) return;
-  for (int w = 1; w < FEW_WAVES; ++w) {
+  for (int w = 1; w < MERGE_WAVES; ++w) {
     sum += sh[(w * 3 + 0) * 64 + lane];
     x += sh[(w * 3 + 1) * 64 + lane];
     y += sh[(w * 3 + 2) * 64 + lane];
@@ -373,7 +72,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void page_merge_few_kernel(PageAttn
 
 template <int BITS, bool BF, int NC>
 static hipError_t launch_few(const PageAttn& a, hipStream_t st) {
-  const size_t lds = FEW_WAVES * NC * (16 * 2 * 4 + 8 * 64 * 16);   // 64.5 KB with two column tiles
+  const size_t lds = few_lds_bytes<NC, FEW_WAVES>();   // 65 KB for each column tile
   static std::atomic<uint64_t> raised{0};
   const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(page_attn_few_kernel<BITS, BF, NC>), raised, lds, LDS_PER_CU);
   if (e != hipSuccess) return e;
@@ -387,9 +86,13 @@ hipError_t launch_page_few(const PageAttn& a, int bits, bool bf, int tiles, hipS
   (tiles == 1 ? (bf ? launch_few<B, true, 1>(a, st) : launch_few<B, false, 1>(a, st)) : (bf ? launch_few<B, true, 2>(a, st) : launch_few<B, false, 2>(a, st)))
   hipError_t e = bits == 16 ? GEAR_FEW(16) : bits == 8 ? GEAR_FEW(8) : GEAR_FEW(4);
 #undef GEAR_FEW
-  if (e != hipSuccess || a.n_split == 1) return e;
+  return e != hipSuccess ? e : merge_page_few(a, bf, st);
+}
+
+hipError_t merge_page_few(const PageAttn& a, bool bf, hipStream_t st) {
+  if (a.n_split == 1) return hipSuccess;
   const unsigned blocks = (unsigned)(a.geom.H * a.few_cols) * (unsigned)a.n_seqs;
-  hipLaunchKernelGGL(page_merge_few_kernel, dim3(blocks), dim3(64 * FEW_WAVES), (size_t)FEW_WAVES * 3 * 64 * 4, st, a, bf ? 1 : 0);
+  hipLaunchKernelGGL(page_merge_few_kernel, dim3(blocks), dim3(64 * MERGE_WAVES), (size_t)MERGE_WAVES * 3 * 64 * 4, st, a, bf ? 1 : 0);
   return hipGetLastError();
 }
 

@@ -16,7 +16,7 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SIMT = os.path.join(ROOT, "tests", "simt")
 CSRC = os.path.join(ROOT, "paper_2403_05527_amd", "csrc")
 PAGES = os.path.join(ROOT, "paper_2403_05527_amd", "csrc_pages")
-SOURCES = ["page_api", "page_copy", "page_few", "page_many"]
+SOURCES = ["page_api", "page_copy", "page_few", "page_many", "page_mixed"]
 
 
 def find_clang():
