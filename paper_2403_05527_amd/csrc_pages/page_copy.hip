@@ -137,7 +137,7 @@ __global__ __launch_bounds__(COPY_THREADS) void page_copy_kernel(PageCopy a) {
   const int64_t slot = (int64_t)t < a.total ? a.slots[t] : -1;
   const bool live = slot >= 0 && slot < (int64_t)g.n_pages << g.shift;   // the same for the 16 lanes of a row
   const int64_t at = live ? slot : 0;
-  const uint64_t keys = (uint64_t)(at >> g.shift) * g.page_bytes + (uint64_t)(2 * h) * g.block_bytes;   // where the head's Keys of the row's page begin
+  const unsigned char* const keys = block_of(g, (int)(at >> g.shift), h, 0);
   const int row = (int)(at & page_mask(g));
   unsigned char* const kp = a.k.data + 2 * (s * a.k.seq + r * a.k.token + h * a.k.head + 8 * c);
   unsigned char* const vp = a.v.data + 2 * (s * a.v.seq + r * a.v.token + h * a.v.head + 8 * c);
@@ -147,12 +147,12 @@ __global__ __launch_bounds__(COPY_THREADS) void page_copy_kernel(PageCopy a) {
       k = *reinterpret_cast<const uint4*>(kp);
       v = *reinterpret_cast<const uint4*>(vp);
     } else {
-      if (a.k.data) k = load_piece<BITS, BF>(g, g.pool + keys, row, c);
-      if (a.v.data) v = load_piece<BITS, BF>(g, g.pool + keys + g.block_bytes, row, c);
+      if (a.k.data) k = load_piece<BITS, BF>(g, keys, row, c);
+      if (a.v.data) v = load_piece<BITS, BF>(g, keys + g.block_bytes, row, c);
     }
   }
   if constexpr (WRITE) {
-    unsigned char* block = const_cast<unsigned char*>(g.pool) + keys;
+    unsigned char* block = const_cast<unsigned char*>(keys);
     store_piece<BITS, BF>(g, block, row, c, k, live);
     store_piece<BITS, BF>(g, block + g.block_bytes, row, c, v, live);
   } else if (live) {

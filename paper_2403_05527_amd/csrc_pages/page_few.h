@@ -172,7 +172,7 @@ __device__ __forceinline__ void few_columns(const PageAttn& a, int bid, unsigned
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const int p = b == 0 ? p0 : p1;
-      const unsigned char* block = g.pool + (uint64_t)(p < 0 ? 0 : p) * g.page_bytes + (uint64_t)(2 * head) * g.block_bytes;
+      const unsigned char* block = block_of(g, p < 0 ? 0 : p, head, 0);
       const uint32_t row0 = (uint32_t)(key + 16 * b) & page_mask(g);
       load_keys<BITS>(x.k[b], g, block, row0, offsets);
       load_values<BITS>(x.v[b], g, block + g.block_bytes, row0, offsets);

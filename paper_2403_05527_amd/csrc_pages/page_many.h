@@ -32,20 +32,33 @@ struct Staged {
   uint4 k[LOADS], v[LOADS];
   uint32_t ksz[LOADS], vsz[LOADS];
 };
+// A lane's places in the wave's rows: of a load's piece and of its word, relative to the first row and its words.
 template <int BITS>
-__device__ __forceinline__ void stage_load(Staged<BITS>& x, const PageGeom& g, const unsigned char* block, uint32_t row0, int lane) {
+struct StageOffsets {
+  uint32_t piece, word;
+};
+template <int BITS>
+__device__ __forceinline__ StageOffsets<BITS> stage_offsets(const PageGeom& g, int lane) {
   using S = Staged<BITS>;
-  const uint32_t piece = lane % S::LANES;
+  const uint32_t piece = lane % S::LANES, row = lane / S::LANES;
+  return StageOffsets<BITS>{row * (16 * BITS) + piece * 16, 4 * ((((piece * S::PIECE) >> g.gshift) << g.shift) + row)};
+}
+template <int BITS>
+__device__ __forceinline__ void stage_load(Staged<BITS>& x, const PageGeom& g, const unsigned char* block, uint32_t row0, const StageOffsets<BITS>& o) {
+  using S = Staged<BITS>;
+  const auto kr = GEAR_BUF_MAKE(block + row0 * (16 * BITS), 16 * (16 * BITS)), vr = GEAR_BUF_MAKE(block + g.block_bytes + row0 * (16 * BITS), 16 * (16 * BITS));
 #pragma unroll
   for (int i = 0; i < S::LOADS; ++i) {
-    const uint32_t row = row0 + i * S::ROWS + lane / S::LANES;
-    const unsigned char* p = block + row * g.row_bytes + piece * 16;
-    x.k[i] = *reinterpret_cast<const uint4*>(p);
-    x.v[i] = *reinterpret_cast<const uint4*>(p + g.block_bytes);
-    if constexpr (BITS < 16) {
-      const unsigned char* w = block + words_at(g) + 4 * ((((piece * S::PIECE) >> g.gshift) << g.shift) + row);
-      x.ksz[i] = *reinterpret_cast<const uint32_t*>(w);
-      x.vsz[i] = *reinterpret_cast<const uint32_t*>(w + g.block_bytes);
+    x.k[i] = GEAR_BUF_LOAD16(kr, o.piece + i * (S::ROWS * 16 * BITS));
+    x.v[i] = GEAR_BUF_LOAD16(vr, o.piece + i * (S::ROWS * 16 * BITS));
+  }
+  if constexpr (BITS < 16) {
+    const uint32_t first = words_at(g) + row0 * 4;
+    const auto kw = GEAR_BUF_MAKE(block + first, g.block_bytes - first), vw = GEAR_BUF_MAKE(block + g.block_bytes + first, g.block_bytes - first);
+#pragma unroll
+    for (int i = 0; i < S::LOADS; ++i) {
+      x.ksz[i] = GEAR_BUF_LOAD4(kw, o.word + i * (S::ROWS * 4));
+      x.vsz[i] = GEAR_BUF_LOAD4(vw, o.word + i * (S::ROWS * 4));
     }
   }
 }
@@ -157,33 +170,41 @@ __device__ __forceinline__ void many_columns(const PageAttn& a, int bid, unsigne
   PageRow pages = page_row(a, s, k1);
   const Biases bs = biases();
   Staged<BITS> next;                       // codes on their way
-  int live = 0, have = 0, have_next = 0;   // of the next tile: the wave's rows that there are; bit w: the keys from 16 w on have a page
+  const StageOffsets<BITS> offsets = stage_offsets<BITS>(g, lane);
+  // Of the next tile: whether all its keys are there, have pages and lie before k1; where not, the wave's rows that are there, and in bit w whether
+  // the keys from 16 w on have a page.
+  bool whole = false, whole_next = false;
+  int live = 16, have = 15, have_next = 15;
+  const int per_tile = MANY_KEYS >> g.shift > 0 ? MANY_KEYS >> g.shift : 1;   // pages
+  const unsigned long long all = (1ull << per_tile) - 1ull;
+  // (kept short: with the four groups' pages looked up one by one it took 800 of a tile's 3750 cycles)
   auto fetch = [&](int key, unsigned char* to) {
-    // (the entries of the tile's four groups of 16 keys lie within four of each other: one look at what the wave holds)
     const int i0 = key >> g.shift;
     if (i0 + 4 > pages.base + 64) load_entries(pages, i0);
-    const int at = key + 16 * wave, left = k1 - key;
-    int page = 0;
-    have_next = 0;
+    const int at = key + 16 * wave;
+    int page = __builtin_amdgcn_readlane(pages.held, (at >> g.shift) - pages.base);
+    whole_next = key + MANY_KEYS <= k1 && ((pages.valid >> (i0 - pages.base)) & all) == all;
+    live = 16;
+    if (!whole_next) {
+      have_next = 0;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const int p = __builtin_amdgcn_readlane(pages.held, ((key + 16 * w) >> g.shift) - pages.base);
-      have_next |= (p >= 0 && 16 * w < left ? 1 : 0) << w;
-      page = w == wave ? p : page;
+      for (int w = 0; w < 4; ++w)
+        have_next |= (__builtin_amdgcn_readlane(pages.held, ((key + 16 * w) >> g.shift) - pages.base) >= 0 && key + 16 * w < k1 ? 1 : 0) << w;
+      live = page < 0 ? 0 : min(16, max(0, k1 - at));
+      page = max(page, 0);
     }
-    live = page < 0 ? 0 : min(16, max(0, k1 - at));
-    const unsigned char* block = g.pool + (uint64_t)max(page, 0) * g.page_bytes + (uint64_t)(2 * head) * g.block_bytes;
+    const unsigned char* block = block_of(g, page, head, 0);
     const uint32_t row0 = (uint32_t)at & page_mask(g);
     if (BITS == 16 && live == 16) {   // straight into LDS: 16 lanes per row, each the piece that belongs at its place
       const auto kb = GEAR_BUF_MAKE(block + row0 * 256, 16 * 256), vb = GEAR_BUF_MAKE(block + g.block_bytes + row0 * 256, 16 * 256);
+      const uint32_t k_at = key_at(lane >> 4, lane & 15), v_at = value_at(lane >> 4, lane & 15);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t row = 4 * i + (lane >> 4);
-        GEAR_DMA16(kb, key_at(row, lane & 15), to + 4096 * wave + 1024 * i);
-        GEAR_DMA16(vb, value_at(row, lane & 15), to + TILE_BYTES + 4096 * wave + 1024 * i);
+      for (int i = 0; i < 4; ++i) {   // rows 4 i + lane / 16
+        GEAR_DMA16(kb, (k_at ^ (64 * i)) + 1024 * i, to + 4096 * wave + 1024 * i);
+        GEAR_DMA16(vb, v_at + 1024 * i, to + TILE_BYTES + 4096 * wave + 1024 * i);
       }
     } else {
-      stage_load<BITS>(next, g, block, row0, lane);
+      stage_load<BITS>(next, g, block, row0, offsets);
       if (BITS == 16) stage_store<BITS, BF>(next, to, to + TILE_BYTES, wave, lane, live, bs);   // (a sequence's last rows)
     }
   };
@@ -202,6 +223,7 @@ __device__ __forceinline__ void many_columns(const PageAttn& a, int bid, unsigne
   int buf = 0;
   for (int key = k0; key < k1; key += MANY_KEYS, buf ^= 1) {
     const bool more = key + MANY_KEYS < k1;
+    whole = whole_next;
     have = have_next;
     const unsigned char* kt = lds + buf * 2 * TILE_BYTES;
     const unsigned char* vt = kt + TILE_BYTES;
@@ -221,7 +243,7 @@ __device__ __forceinline__ void many_columns(const PageAttn& a, int bid, unsigne
     if (more) fetch(key + MANY_KEYS, lds + (buf ^ 1) * 2 * TILE_BYTES);
     if (busy) {
       // keys 32 b + 8 (i / 4) + 4 half + i % 4 of the tile
-      const bool edge = key + MANY_KEYS > all_see || have != 15;
+      const bool edge = key + MANY_KEYS > all_see || !whole;
       if (edge) {
         int first = key + 4 * half;
         GEAR_PIN_VGPR(first);   // (what depends on it stays in here)
@@ -229,7 +251,7 @@ __device__ __forceinline__ void many_columns(const PageAttn& a, int bid, unsigne
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            if (first + 32 * b + 8 * (i >> 2) + (i & 3) >= sees || ((have >> (2 * b + (i >> 3))) & 1) == 0) sc[b][i] = -INFINITY;
+            if (first + 32 * b + 8 * (i >> 2) + (i & 3) >= sees || (!whole && ((have >> (2 * b + (i >> 3))) & 1) == 0)) sc[b][i] = -INFINITY;
           }
       }
       float top = -INFINITY;

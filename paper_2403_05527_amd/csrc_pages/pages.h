@@ -55,7 +55,7 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 // The pool as the kernels see it.
 struct PageGeom {
   const unsigned char* pool;
-  uint64_t page_bytes;
+  uint32_t page_bytes;    // below 2^31
   uint32_t block_bytes;   // Keys or Values of one head in a page
   uint32_t row_bytes;
   int32_t n_pages;
@@ -64,6 +64,10 @@ struct PageGeom {
   int32_t H;
 };
 __host__ __device__ inline uint32_t page_mask(const PageGeom& g) { return (1u << g.shift) - 1u; }
+// where a head's Keys (tensor 0) or Values (1) begin in a page
+__device__ __forceinline__ const unsigned char* block_of(const PageGeom& g, int page, int head, int tensor) {
+  return g.pool + ((uint64_t)(uint32_t)page * g.page_bytes + (uint32_t)(2 * head + tensor) * g.block_bytes);
+}
 __host__ __device__ inline uint32_t words_at(const PageGeom& g) { return g.row_bytes << g.shift; }   // the (scale, zero) words in a block
 
 // 16-bit rows with strides in elements
@@ -240,15 +244,17 @@ __device__ __forceinline__ int row_sees(const PageAttn& a, const SeqSpan& s, int
 struct PageRow {
   const int32_t* table;
   int32_t base, held, n_pages, shift, end;   // `end`: no key from there on is asked for
+  unsigned long long valid;                  // bit i: entry base + i is a page
 };
 __device__ __forceinline__ PageRow page_row(const PageAttn& a, int s, int end) {
-  return PageRow{a.table + (int64_t)s * a.width, -64, 0, a.geom.n_pages, a.geom.shift, end};
+  return PageRow{a.table + (int64_t)s * a.width, -64, 0, a.geom.n_pages, a.geom.shift, end, 0ull};
 }
 __device__ __forceinline__ void load_entries(PageRow& r, int i) {   // from entry i on, which is one of a key before `end`; behind the last: that one
   r.base = i;
   const int at = i + lane_id(), last = (r.end - 1) >> r.shift;
   const int p = r.table[at <= last ? at : last];
   r.held = p >= 0 && p < r.n_pages ? p : -1;
+  r.valid = __ballot(r.held >= 0);
 }
 // The page of a key (the same in all lanes of the wave); -1: none.  Keys are asked for in ascending order.
 __device__ __forceinline__ int page_of(PageRow& r, int key) {
