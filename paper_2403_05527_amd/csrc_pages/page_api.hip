@@ -4,28 +4,29 @@
 
 namespace gear {
 
+constexpr size_t RECORD_BYTES = (2 + D) * sizeof(float);   // of one column and part
 #ifndef GEAR_PAGE_CUS   // (the CPU stand-in sets it, so that its small cases are divided)
 #define GEAR_PAGE_CUS GEAR_CUS
 #endif
 constexpr int FEW_COLS_MOST = 32;
-// Blocks of the few-column kernel that the chip holds at once, with one tile of columns; records' rows x parts are bounded by twice that.
-constexpr int FEW_SLOTS = 2 * GEAR_PAGE_CUS, FEW_BLOCKS_MOST = 2 * FEW_SLOTS, MANY_SLOTS = 2 * GEAR_PAGE_CUS;
+// Blocks of either kernel that the chip holds at once (of few columns: with one tile of them, with two half as many), and the most that dividing the
+// keys makes of fewer: they bound the records, 64 MB of both kinds.
+constexpr int FEW_SLOTS = 2 * GEAR_PAGE_CUS, MANY_SLOTS = 2 * GEAR_PAGE_CUS;
+constexpr int FEW_BLOCKS_MOST = FEW_SLOTS * 3 / 2, MANY_BLOCKS_MOST = MANY_SLOTS * 3 / 2;
 
-// Parts of the key axis for `blocks` (sequence, head) pairs of up to max_kv tokens and `cols` columns: the best number of equal parts by a
-// model in ns.  A block takes 4000 (its launch, the first loads, the joining of its waves) and 8 per token (the chain of a wave's steps, by eight
-// waves); all of them together no less than their bytes at 6 TB/s; with more than one part the merge takes 3500, the launch of a wave per four records and their bytes
-// at 5 TB/s.  1 x 8 heads x 32768 tokens at 4 bits: 21.2 us in 96 parts of 341 tokens, 18.3 in 64 with the merge, 19.6 in 32; 33 sequences x 8 heads of 600 to 4000
-// tokens: 46 us undivided, 41 and 15 of merging in three parts.
-static int few_parts(int64_t blocks, int cols, int max_kv, int bytes_per_key, int slots) {
-  const int by_keys = max_kv / FEW_PART;
-  const int64_t by_blocks = blocks > 0 ? FEW_BLOCKS_MOST / blocks : 1;
-  const int most = (int)(by_blocks < by_keys ? by_blocks : by_keys);
-  const double bytes = (double)blocks * max_kv * bytes_per_key / 6000.0;
+// The number of equal parts of the key axis that a model finds the fastest, in ns: `blocks` of them undivided on `slots` places, each taking `once` and
+// per token `chain`; all together no less than `bytes` (the memory's share); with more than one part, a merge whose records (`records` bytes per part) are
+// written and read at 5 TB/s.  A quarter of the lesser of the two bounds is added: blocks of unequal length.
+// filled: parts have a length, not a number, so sequences shorter than max_kv make fewer; but no more than 86 % of the slots count, since blocks that end at once
+// leave the XCDs unevenly filled (504 parts on 512 slots: the last dozen began when the first had ended).
+static int best_parts(int64_t blocks, double filled, int slots, int most_blocks, int max_kv, int least_part, double once, double chain, double bytes, double records) {
+  const int64_t by_blocks = blocks > 0 ? most_blocks / blocks : 1;
+  const int by_keys = max_kv / least_part, most = (int)(by_blocks < by_keys ? by_blocks : by_keys);
   int best = 1;
   double least = 0.0;
   for (int n = 1; n <= most; ++n) {
-    const double chain = (double)((blocks * n + slots - 1) / slots) * (4000.0 + 8.0 * max_kv / n);
-    const double t = (chain > bytes ? chain : bytes) + (n > 1 ? 3500.0 + 20.0 * n + (double)blocks * cols * n * 1040.0 / 5000.0 : 0.0);
+    const double time = std::ceil((n > 1 ? filled / 0.86 : 1.0) * (double)(blocks * n) / slots) * (once + chain * max_kv / n);
+    const double t = (time > bytes ? time + 0.25 * bytes : bytes + 0.25 * time) + (n > 1 ? 4000.0 + 20.0 * n + records * n * 2.0 / 5000.0 : 0.0);
     if (n == 1 || t < least) {
       best = n;
       least = t;
@@ -45,16 +46,22 @@ PagePlan page_plan(int H, int gq, int n_seqs, int n_tokens, int max_q, int max_k
   p.few_limit = !p.few ? 0 : all_few ? (int)cols : gq <= 16 ? 16 : FEW_COLS_MOST;
   p.few_tiles = p.few_limit <= 16 ? 1 : 2;
   p.few_split = p.many_split = 1;
+  const double filled = n_seqs >= 4 ? 0.75 : 1.0;
   if (p.few) {
-    p.few_split = few_parts((int64_t)n_seqs * H, p.few_limit, max_kv, bytes_per_key, p.few_tiles == 1 ? FEW_SLOTS : FEW_SLOTS / 2);
+    // A block of eight waves: 4 us (its launch, the first loads, the joining of its waves) and 8 ns per token (a wave's chain of steps).  1 x 8 heads x 32768 tokens
+    // at 4 bits: 21.2 us in 96 parts, 16.7 in 64, 18.2 in 32; 33 sequences of 600 to 4000 tokens, 264 blocks: 46 us undivided, 41 and 15 of merging in
+    // three parts.
+    const int64_t blocks = (int64_t)n_seqs * H;
+    p.few_split = best_parts(blocks, filled, p.few_tiles == 1 ? FEW_SLOTS : FEW_SLOTS / 2, FEW_BLOCKS_MOST, max_kv, FEW_PART, 4000.0, 8.0,
+                             (double)blocks * max_kv * bytes_per_key / 6000.0, (double)blocks * p.few_limit * RECORD_BYTES);
     if (p.few_split > 1) p.few_rows = (int64_t)n_seqs * H * p.few_limit;
   }
   if (p.many) {
-    // As many parts as fill the slots once.  Not more, even where the sequences differ: three chunks of 483 to 566 tokens behind up to 2900, 416 blocks,
-    // take 100 us in one part each and 140 in two, of which 18 go to joining the records (35 MB each way).
-    const int64_t blocks = ((int64_t)n_tokens * gq + MANY_COLS - 1) / MANY_COLS * H, by_slots = blocks > 0 ? MANY_SLOTS / blocks : 1;
-    const int64_t by_keys = max_kv / MANY_PART, n = by_slots < by_keys ? by_slots : by_keys;
-    p.many_split = n < 1 ? 1 : (int)n;
+    // A block: 6 us and 2 us per tile of 64 tokens.  Four chunks of 512 tokens behind 4096, 512 blocks: 182 us undivided, and two parts would take 34 for their records
+    // alone; three chunks of 483 to 566 behind up to 2900, 416 blocks: 100 us undivided, 140 in two parts.
+    const int64_t tiles = uniform ? (cols + MANY_COLS - 1) / MANY_COLS * n_seqs : ((int64_t)n_tokens * gq + MANY_COLS - 1) / MANY_COLS;
+    const int64_t rows = (int64_t)n_tokens * H * gq;
+    p.many_split = best_parts(tiles * H, filled, MANY_SLOTS, MANY_BLOCKS_MOST, max_kv, MANY_PART, 6000.0, 2000.0 / MANY_KEYS, 0.0, (double)rows * RECORD_BYTES);
     p.many_least = max_kv / p.many_split > MANY_PART ? max_kv / p.many_split : MANY_PART;
     if (p.many_split > 1) p.many_rows = (int64_t)n_tokens * H * gq;
   }
@@ -76,7 +83,7 @@ int64_t page_records_most(int H, int gq, int n_seqs, int n_tokens, int max_q, in
     few = blocks * few_cols;
   }
   if ((int64_t)max_q * gq > FEW_COLS_MOST && max_kv / MANY_PART > 1) {
-    const int64_t by_keys = (int64_t)n_tokens * H * gq * (max_kv / MANY_PART), by_slots = (int64_t)MANY_SLOTS * MANY_COLS;
+    const int64_t by_keys = (int64_t)n_tokens * H * gq * (max_kv / MANY_PART), by_slots = (int64_t)MANY_BLOCKS_MOST * MANY_COLS;
     many = by_keys < by_slots ? by_keys : by_slots;
   }
   return few + many;
@@ -88,7 +95,6 @@ using namespace gear;
 
 namespace {
 
-constexpr size_t RECORD_BYTES = (2 + D) * sizeof(float);
 constexpr int64_t INT_MOST = 0x7FFFFFFF;
 
 int check_page_config(const gear_page_config* c, size_t* pool_bytes, PageGeom* g) {

@@ -1,6 +1,7 @@
 // Attention of many query columns over pages (page_many.h): the launch, and the joining of the parts.
 #include "page_launch.h"
 #include "page_many.h"
+#include "page_merge.h"
 
 namespace gear {
 
@@ -11,11 +12,13 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_many_kernel(PageAtt
   many_columns<BITS, BF>(a, (int)blockIdx.x, lds);
 }
 
-// The records of a row's parts become its output (see page_merge_few_kernel): one wave per token and query head.
+// The records of a row's parts become its output (see page_merge_few_kernel): WAVES waves per token and query head, eight records of each on their way.
+template <int WAVES>
 __global__ __launch_bounds__(256) void page_merge_many_kernel(PageAttn a, int bf) {
+  GEAR_DYN_LDS(lds);
   const PageGeom& g = a.geom;
-  const int lane = lane_id(), Hq = g.H * a.gq;
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = lane_id(), Hq = g.H * a.gq, wave = (int)(threadIdx.x >> 6), mine = WAVES == 1 ? 0 : wave;
+  const int64_t id = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
   const int token = (int)(id / Hq), jq = (int)(id - (int64_t)token * Hq), head = jq / a.gq;
   int s = -1;
   for (int base = 0; base < a.n_seqs; base += 64) {
@@ -28,23 +31,10 @@ __global__ __launch_bounds__(256) void page_merge_many_kernel(PageAttn a, int bf
   const int row = token - sp.q0, cols = sp.nq * a.gq;
   if (row < 0 || row >= sp.nq || (sp.nq <= a.few && cols <= a.few)) return;
   const int col = row * a.gq + (jq - head * a.gq), last = min(col / MANY_COLS * MANY_COLS + MANY_COLS, cols) - 1;
-  const Parts parts = parts_of(row_sees(a, sp, last / a.gq), a.n_split, a.least, MANY_KEYS);
-  if (parts.count <= 1) return;
-  const int64_t rec = id * a.n_split;
-  float top = -INFINITY;
-  for (int i = 0; i < parts.count; ++i) top = fmaxf(top, a.rec_ml[rec + i].x);
-  const float from = top == -INFINITY ? 0.0f : top;
-  float sum = 0.0f, x = 0.0f, y = 0.0f;
-  for (int i = 0; i < parts.count; ++i) {
-    const float2 ml = a.rec_ml[rec + i], v = *reinterpret_cast<const float2*>(a.rec_o + (rec + i) * D + 2 * lane);
-    const float by = GEAR_EXP2(ml.x - from);
-    sum += ml.y * by;
-    x += v.x * by;
-    y += v.y * by;
-  }
-  const float r = sum > 0.0f ? 1.0f / sum : 0.0f;
-  unsigned char* p = a.out.data + 2 * ((int64_t)token * a.out.token + (int64_t)jq * a.out.head + 2 * lane);
-  *reinterpret_cast<uint32_t*>(p) = bf ? pack2<true>(x * r, y * r) : pack2<false>(x * r, y * r);
+  const int count = parts_of(row_sees(a, sp, last / a.gq), a.n_split, a.least, MANY_KEYS).count;
+  if (count <= 1) return;
+  const Merged x = merge_records<WAVES>(a, id * a.n_split, count, mine, lane, reinterpret_cast<float*>(lds));
+  if (mine == 0) store_merged(a, x, token, jq, lane, bf);
 }
 
 template <int BITS, bool BF>
@@ -64,7 +54,10 @@ hipError_t launch_page_many(const PageAttn& a, int bits, bool bf, hipStream_t st
 hipError_t merge_page_many(const PageAttn& a, bool bf, hipStream_t st) {
   if (a.n_split == 1) return hipSuccess;
   const int64_t rows = (int64_t)a.n_tokens * a.geom.H * a.gq;
-  hipLaunchKernelGGL(page_merge_many_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, bf ? 1 : 0);
+  if (a.n_split <= 8)
+    hipLaunchKernelGGL(page_merge_many_kernel<1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, bf ? 1 : 0);
+  else
+    hipLaunchKernelGGL(page_merge_many_kernel<4>, dim3((unsigned)rows), dim3(256), (size_t)MERGE_LDS, st, a, bf ? 1 : 0);
   return hipGetLastError();
 }
 
