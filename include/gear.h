@@ -276,7 +276,7 @@ typedef struct gear_page_rows {
 typedef struct gear_page_batch {
   int32_t n_seqs;
   int32_t n_tokens;             /* rows of q and out (those outside every sequence are not touched)   */
-  int32_t max_q;                /* no sequence has more new tokens; rows beyond that are not computed */
+  int32_t max_q;                /* no sequence has more new tokens (the rows of one that has may stay)  */
   int32_t max_kv;               /* about the longest sequence: what the work is divided by            */
   int32_t table_width;          /* entries of a sequence's row of page_table                          */
   int32_t causal;               /* 0: every row sees all kv_len tokens                                */

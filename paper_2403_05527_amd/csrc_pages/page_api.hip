@@ -95,7 +95,7 @@ using namespace gear;
 
 namespace {
 
-constexpr int64_t INT_MOST = 0x7FFFFFFF;
+constexpr int64_t INT_MOST = 0x7FFFFFFF, THREADS_MOST = 0xFFFFFFFF;   // of a launch
 
 int check_page_config(const gear_page_config* c, size_t* pool_bytes, PageGeom* g) {
   if (!c) return GEAR_EINVAL;
@@ -154,7 +154,7 @@ int copy_rows(const gear_page_config* cfg, const void* pool, size_t pool_bytes, 
   if (total == 0) return GEAR_OK;
   if (!slots) return GEAR_EINVAL;
   if (misaligned(slots, 8)) return GEAR_EALIGN;
-  if (total > INT_MOST - 4096 || (total + 15) / 16 * cfg->H_kv > INT_MOST) return GEAR_ECAPACITY;
+  if (total > INT_MOST - 4096 || (total + 15) / 16 * cfg->H_kv > THREADS_MOST / 256) return GEAR_ECAPACITY;
   return launch_page_copy(g, cfg->bits, cfg->dtype == GEAR_BF16, write, view_of(K), view_of(V), slots, n_seqs, n_rows,
                           static_cast<hipStream_t>(stream)) == hipSuccess ? GEAR_OK : GEAR_EHIP;
 }
@@ -223,7 +223,7 @@ int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_by
     if (workspace_bytes < RECORD_BYTES * (size_t)(few_recs + many_recs)) return GEAR_ECAPACITY;
   }
   const int64_t tiles = (int64_t)b.n_tokens * gq / MANY_COLS + b.n_seqs;
-  if ((int64_t)b.n_seqs * H * p.few_split + tiles * H * p.many_split > INT_MOST) return GEAR_ECAPACITY;
+  if ((int64_t)b.n_seqs * H * p.few_split + tiles * H * p.many_split > THREADS_MOST / 512) return GEAR_ECAPACITY;
 
   a.q_start = b.q_start;
   a.kv_len = b.kv_len;

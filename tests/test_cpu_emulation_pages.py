@@ -74,6 +74,10 @@ CASES = [
     Case("many_bf16_4", BF16, 4, 32, 16, 1, 1, [(34, 131)], bad=True),
     Case("many_split", F16, 16, 128, 64, 1, 1, [(36, 1100)], max_kv=1100),
     Case("mixed", F16, 8, 64, 16, 1, 4, [(1, 60), (50, 90), (0, 0), (3, 30)], pad=1),
+    Case("mixed_two_launches", F16, 16, 128, 16, 1, 2, [(1, 60), (33, 90), (2, 30)], max_kv=1000000),
+    Case("mixed_two_tiles", BF16, 4, 64, 16, 1, 20, [(1, 40), (3, 50)], bad=True),
+    Case("merge_many_parts", F16, 4, 32, 16, 1, 1, [(33, 1300)], max_kv=1300),
+    Case("many_sequences", F16, 8, 128, 16, 1, 1, [(1 + 33 * (i == 5), 17 + i % 3 + 33 * (i == 5)) for i in range(66)]),
     Case("empty_many", F16, 16, 128, 16, 1, 1, [(70, 20)]),
     Case("negative_scale", BF16, 16, 128, 16, 1, 2, [(1, 40), (40, 60)], scale=-0.05),
     Case("write_f16", F16, 16, 128, 16, 2, 1, [(0, 19)], write=True),

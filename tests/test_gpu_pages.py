@@ -94,6 +94,9 @@ SHAPES = [   # page, H, gq, sequences (new tokens, tokens), padding rows
     (16, 1, 4, [(1, 60), (50, 90), (0, 0), (3, 30), (100, 1300)], 3),   # single tokens among chunks
     (16, 1, 1, [(70, 20), (9, 4), (33, 0)], 0),                # rows that see nothing
     (16, 1, 40, [(1, 50), (2, 33)], 0),                        # more query heads than a few-column tile
+    (16, 1, 20, [(1, 70), (40, 90), (2, 33), (1, 16)], 1),     # ... than one of its tiles, beside a chunk
+    (32, 2, 1, [(1 + (i % 7 == 3) * 40, 50 + i) for i in range(70)], 0),   # more sequences than a wave has lanes
+    (16, 1, 2, [(70, 1500), (90, 90), (65, 800), (200, 3000)], 0),          # chunks of unequal length whose keys are divided
 ]
 
 
@@ -161,6 +164,17 @@ def test_large_scores():
                 c.q = torch.ones_like(c.q)
                 c.pool = torch.stack([pg.pack(x, 16, 128, dtype) for x in (c.K, c.V)], 2).reshape(-1).to(DEV)
                 c.check(attn(c, scale=0.7), scale=0.7)
+
+
+@pytest.mark.parametrize("form", [FORMS[0], FORMS[4], FORMS[5]], ids=FORM_IDS)
+@pytest.mark.parametrize("max_kv", [1, 700, 20000, 10 ** 6])
+def test_bounds_that_are_not_met(form, max_kv):
+    """max_kv sizes the launch and nothing else: far too small, far too large (single tokens and chunks then go in two launches), and a batch whose
+    n_tokens looks like one of equal sequences."""
+    dtype, bits, group = form
+    for seqs, pad, max_q in (([(1, 700), (40, 640), (3, 65)], 0, None), ([(1, 700), (2, 30)], 0, 3), ([(1, 60), (0, 9), (40, 640), (39, 200)], 40, None)):
+        c = Cache(dtype, bits, group, 16, 1, 2, seqs, seed=len(seqs), pad=pad)
+        c.check(attn(c, max_kv=max_kv, max_q=max_q), before=77.0)
 
 
 def test_random_batches():
