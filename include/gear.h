@@ -292,7 +292,7 @@ int gear_page_bytes(const gear_page_config* cfg, size_t* pool_bytes);
  * Writes row (s, t, h) of K and V into slot slots[s * n_rows + t] of head h, for all s < n_seqs, t < n_rows.
  * slots     : device int64.  A slot outside 0 .. n_pages * page_size - 1 (-1: padding) is skipped.  A slot
  *             should be named once: of one that is named twice the bytes may come from either row.
- * Values must be finite, and below 2^126 in magnitude where they are quantized.
+ * Values must be finite, and below 2^100 in magnitude where they are quantized (bf16 reaches further).
  */
 int gear_page_write(const gear_page_config* cfg, void* pool, size_t pool_bytes, const gear_page_rows* K,
                     const gear_page_rows* V, int32_t n_seqs, int32_t n_rows, const int64_t* slots, void* stream);

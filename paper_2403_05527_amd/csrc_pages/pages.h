@@ -99,20 +99,20 @@ __device__ __forceinline__ floatx16 mfma32(const uint4& a, const uint4& b, const
 }
 
 // ---- codes to values ----------------------------------------------------------
-// Two codes as integers in the halves of a word, as the arithmetic of the type wants them: fp16 has them as 1024 + code or 64 + code
-// (the low mantissa bits of those numbers), bf16 goes through fp32.
+// Two codes as integers in the halves of a word; fp16 arithmetic has them as 1024 + code or 64 + code (the low mantissa bits of those numbers), bf16 goes
+// through fp32.
 // (scale, zero) words of the two entries: `sz0` for the low one.  The same word twice where both lie in one group of a row.
 struct PairScale {
   uint32_t scale, zero;   // fp16: a pair each
-  float s0, z0, s1, z1;   // bf16
+  float s0, z0, s1, z1;   // bf16; the scales times 2^24
 };
 template <bool BF>
 __device__ __forceinline__ PairScale pair_scale(uint32_t sz0, uint32_t sz1) {
   PairScale p;
   if constexpr (BF) {
-    p.s0 = __uint_as_float(sz0 << 16);
+    p.s0 = __uint_as_float(sz0 << 16) * 16777216.0f;
     p.z0 = __uint_as_float(sz0 & 0xFFFF0000u);
-    p.s1 = __uint_as_float(sz1 << 16);
+    p.s1 = __uint_as_float(sz1 << 16) * 16777216.0f;
     p.z1 = __uint_as_float(sz1 & 0xFFFF0000u);
   } else {
     p.scale = GEAR_BYTE_PERM(sz1, sz0, 0x05040100u);
@@ -137,8 +137,10 @@ __device__ __forceinline__ uint32_t value_f16(uint32_t biased, uint32_t neg_bias
   const uint32_t c = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2_t, biased) + __builtin_bit_cast(h2_t, neg_bias));
   return GEAR_PK_FMA_F16(c, p.scale, p.zero);
 }
-__device__ __forceinline__ uint32_t value_bf16(uint32_t c0, uint32_t c1, const PairScale& p) {
-  return GEAR_PACK_BF2(__builtin_fmaf((float)c0, p.s0, p.z0), __builtin_fmaf((float)c1, p.s1, p.z1));
+// bf16: value pair of two codes in the halves of a word.  As fp16 numbers those are denormals, code * 2^-24, which one instruction takes into an fp32
+// multiply-add (the scales of a pair are 2^24 times theirs): a product and a sum, rounded to fp32 and then to bf16.
+__device__ __forceinline__ uint32_t value_bf16(uint32_t codes, float s0, float z0, float s1, float z1) {
+  return GEAR_PACK_BF2(__builtin_fmaf(h2f(codes & 0xFFFFu), s0, z0), __builtin_fmaf(h2f(codes >> 16), s1, z1));
 }
 // Channels 2 i, 2 i + 1 (i = 0..3) of a run of eight along a row: w0, w1 are the run's code words (w1 at 8 bits only).
 template <int BITS, bool BF>
@@ -146,13 +148,14 @@ __device__ __forceinline__ uint32_t row_pair(uint32_t w0, uint32_t w1, int i, co
   if constexpr (BITS == 8) {
     const uint32_t w = i < 2 ? w0 : w1;
     if constexpr (BF) {
-      return value_bf16((w >> (16 * (i & 1))) & 0xFFu, (w >> (16 * (i & 1) + 8)) & 0xFFu, p);
+      return value_bf16(GEAR_BYTE_PERM(0u, w, (i & 1) ? 0x0C030C02u : 0x0C010C00u), p.s0, p.z0, p.s1, p.z1);
     } else {
       return value_f16(GEAR_BYTE_PERM(BYTES_64H, w, (i & 1) ? 0x04030402u : 0x04010400u), F16_NEG_1024, p);
     }
   } else {   // 4 bits: nibble i of each half
     if constexpr (BF) {
-      return value_bf16((w0 >> (4 * i)) & 0xFu, (w0 >> (4 * i + 16)) & 0xFu, p);
+      const uint32_t x = i < 2 ? w0 : w0 >> 8;   // (the upper nibble of a byte stays where it is: 16 code, with a 16th of the scale)
+      return (i & 1) ? value_bf16(x & 0x00F000F0u, p.s0 * 0.0625f, p.z0, p.s1 * 0.0625f, p.z1) : value_bf16(x & 0x000F000Fu, p.s0, p.z0, p.s1, p.z1);
     } else {
       const uint32_t x = i < 2 ? w0 : w0 >> 8;
       return (i & 1) ? value_f16((x & 0x00F000F0u) | bs.b64, F16_NEG_64, p) : value_f16((x & 0x000F000Fu) | bs.b1024, F16_NEG_1024, p);
@@ -183,7 +186,7 @@ __device__ __forceinline__ uint32_t column_pair(const uint32_t* x, const uint32_
     return GEAR_BYTE_PERM(y[e >> 1], x[e >> 1], (e & 1) ? 0x07060302u : 0x05040100u);
   } else if constexpr (BITS == 8) {
     const uint32_t w = (e & 2) ? y[e >> 2] : x[e >> 2];
-    if constexpr (BF) return value_bf16((w >> (16 * (e & 1))) & 0xFFu, (w >> (16 * (e & 1) + 8)) & 0xFFu, p);
+    if constexpr (BF) return value_bf16(GEAR_BYTE_PERM(0u, w, (e & 1) ? 0x0C030C02u : 0x0C010C00u), p.s0, p.z0, p.s1, p.z1);
     else return value_f16(GEAR_BYTE_PERM(BYTES_64H, w, (e & 1) ? 0x04030402u : 0x04010400u), F16_NEG_1024, p);
   } else {
     return row_pair<4, BF>((e & 1) ? y[0] : x[0], 0u, e >> 1, p, bs);   // (nibble e / 2 of each half)
