@@ -9,7 +9,7 @@ namespace gear {
 template <int BITS, bool BF>
 __global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_many_kernel(PageAttn a) {
   GEAR_DYN_LDS(lds);
-  many_columns<BITS, BF>(a, (int)blockIdx.x, lds);
+  many_columns<BITS, BF, true>(a, (int)blockIdx.x, lds);
 }
 
 // The records of a row's parts become its output (see page_merge_few_kernel): WAVES waves per token and query head, eight records of each on their way.

@@ -13,7 +13,7 @@ template <int BITS, bool BF, int NC>
 __global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_mixed_kernel(PageAttn many, PageAttn few, int many_blocks) {
   GEAR_DYN_LDS(lds);
   const int bid = (int)blockIdx.x;
-  if (bid < many_blocks) many_columns<BITS, BF>(many, bid, lds);
+  if (bid < many_blocks) many_columns<BITS, BF, false>(many, bid, lds);
   else few_columns<BITS, BF, NC, MIXED_WAVES>(few, bid - many_blocks, lds);
 }
 

@@ -68,6 +68,7 @@ inline hipError_t hipGetSymbolAddress(void** p, const void* sym) { *p = const_ca
 #define GEAR_LDS_DRAIN() simt::wave_barrier()
 #define GEAR_DMA_BARRIER() pthread_barrier_wait(&simt::block_bar)
 #define GEAR_WAVE_UNIFORM(x) (x)
+#define GEAR_WAVE_PRIO(p) ((void)0)
 #define GEAR_BYTE_PERM(hi, lo, sel) simt_byte_perm((hi), (lo), (sel))
 #define GEAR_FMED3(x, lo, hi) fminf(fmaxf((x), (lo)), (hi))
 #define GEAR_FDOT2(a, b, c) simt_fdot2((a), (b), (c))
