@@ -292,7 +292,8 @@ int gear_page_bytes(const gear_page_config* cfg, size_t* pool_bytes);
  * Writes row (s, t, h) of K and V into slot slots[s * n_rows + t] of head h, for all s < n_seqs, t < n_rows.
  * slots     : device int64.  A slot outside 0 .. n_pages * page_size - 1 (-1: padding) is skipped.  A slot
  *             should be named once: of one that is named twice the bytes may come from either row.
- * Values must be finite, and below 2^100 in magnitude where they are quantized (bf16 reaches further).
+ * Values must be finite and, where they are quantized, below 2^16 - 128 (fp16; a code of one beyond may stand
+ * for an infinity) or 2^100 (bf16) in magnitude.
  */
 int gear_page_write(const gear_page_config* cfg, void* pool, size_t pool_bytes, const gear_page_rows* K,
                     const gear_page_rows* V, int32_t n_seqs, int32_t n_rows, const int64_t* slots, void* stream);

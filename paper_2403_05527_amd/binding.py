@@ -300,7 +300,7 @@ def make_page_batch(q_start, kv_len, page_table, n_tokens, max_q, max_kv, causal
     d = _page_device()
     b = gear_page_batch(n, n_tokens, max_q, max_kv, width, 1 if causal else 0, _page_index(q_start, torch.int32, n + 1, d, "q_start"),
                         _page_index(kv_len, torch.int32, n, d, "kv_len"), _page_index(page_table, torch.int32, n * width, d, "page_table"))
-    b.tensors = (q_start, kv_len, page_table)
+    b.tensors, b.device = (q_start, kv_len, page_table), d
     return b
 
 
@@ -312,6 +312,8 @@ def gear_page_attn_bytes(cfg, H_q, batch):
 
 def gear_page_attn(cfg, pool, batch, q, out, scale, workspace):
     device = _page_device()
+    if getattr(batch, "device", device) != device:
+        raise ValueError("the batch's lengths and page table lie on cuda:%d, not on the current GPU" % batch.device)
     H_q = q.shape[-2]
     a, seqs, n = _page_rows(q, cfg, H_q, device, "q")
     b, seqs_out, n_out = _page_rows(out, cfg, H_q, device, "out")

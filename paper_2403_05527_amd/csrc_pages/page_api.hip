@@ -149,9 +149,9 @@ int copy_rows(const gear_page_config* cfg, const void* pool, size_t pool_bytes, 
   if (rc) return rc;
   if (n_seqs < 0 || n_rows < 0 || (write ? !K || !V : !K && !V)) return GEAR_EINVAL;
   const int64_t total = (int64_t)n_seqs * n_rows;
+  if (total == 0) return GEAR_OK;   // (tensors without an entry have no address)
   if (K && (rc = check_rows(K, n_seqs, n_rows, cfg->H_kv, !write))) return rc;
   if (V && (rc = check_rows(V, n_seqs, n_rows, cfg->H_kv, !write))) return rc;
-  if (total == 0) return GEAR_OK;
   if (!slots) return GEAR_EINVAL;
   if (misaligned(slots, 8)) return GEAR_EALIGN;
   if (total > INT_MOST - 4096 || (total + 15) / 16 * cfg->H_kv > THREADS_MOST / 256) return GEAR_ECAPACITY;
@@ -208,10 +208,11 @@ int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_by
   int rc = check_pool(cfg, pool, pool_bytes, &a.geom);
   if (rc || (rc = check_batch(cfg, H_q, batch))) return rc;
   const gear_page_batch& b = *batch;
-  if (!q || !out || !std::isfinite(scale)) return GEAR_EINVAL;
-  if ((rc = check_rows(q, 1, b.n_tokens, H_q, false)) || (rc = check_rows(out, 1, b.n_tokens, H_q, true))) return rc;
+  const float scale_log2 = std::fabs(scale) * 1.44269504088896340736f;
+  if (!q || !out || !std::isfinite(scale_log2) || b.table_width < 0) return GEAR_EINVAL;
   if (b.n_seqs == 0 || b.n_tokens == 0 || b.max_q == 0) return GEAR_OK;
-  if (!b.q_start || !b.kv_len || b.table_width < 0 || (b.table_width > 0 && !b.page_table)) return GEAR_EINVAL;
+  if ((rc = check_rows(q, 1, b.n_tokens, H_q, false)) || (rc = check_rows(out, 1, b.n_tokens, H_q, true))) return rc;
+  if (!b.q_start || !b.kv_len || (b.table_width > 0 && !b.page_table)) return GEAR_EINVAL;
   if (misaligned(b.q_start, 4) || misaligned(b.kv_len, 4) || misaligned(b.page_table, 4) || misaligned(workspace, 16)) return GEAR_EALIGN;
   if ((int64_t)b.table_width * cfg->page_size > INT_MOST - 1024) return GEAR_ECAPACITY;
   const int H = cfg->H_kv, gq = H_q / H;
@@ -230,7 +231,7 @@ int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_by
   a.table = b.page_table;
   a.q = view_of(q);
   a.out = view_of(out);
-  a.scale_log2 = std::fmax(std::fabs(scale) * 1.44269504088896340736f, 1e-37f);   // (a scale of 0: every score comes to less than a step of 2^0)
+  a.scale_log2 = std::fmax(scale_log2, 1e-37f);   // (a scale of 0: every score comes to less than a step of 2^0)
   a.flip = scale < 0.0f ? 0x80008000u : 0u;
   a.width = b.table_width;
   a.n_seqs = b.n_seqs;

@@ -389,3 +389,22 @@ def test_a_pool_past_four_gigabytes():
         gb.gear_page_attn(cfg, pool, b, q[:m].to(DEV), out, 0.1, torch.empty(1 << 24, dtype=torch.uint8, device=DEV))
         want, bound = pg.attend(q[:m], Kp, Vp, [0, m], [n], [[0, 1]], 0.1, True)
         assert bool(((out.cpu().double() - want).abs() <= bound).all())
+
+
+def test_calls_of_no_rows():
+    """Tensors without an entry: nothing to do, and nothing is touched."""
+    pool = gb.PagePool(gb.make_page_config(2, 16, 2, 16, dtype=F16), DEV)
+    K, V = (torch.randn(4, 2, 128, device=DEV, dtype=F16) for _ in range(2))
+    slots = torch.arange(4, device=DEV)
+    pool.write(K, V, slots)
+    before = pool.pool.clone()
+    pool.write(K[:0], V[:0], slots[:0])
+    Kb, Vb = pool.read(slots[None, :0])
+    assert Kb.shape == Vb.shape == (1, 0, 2, 128) and torch.equal(pool.pool, before)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    q = torch.randn(1, 2, 128, device=DEV, dtype=F16)
+    table = i32(0).view(1, 1)
+    assert pool.attn(q[:0], gb.make_page_batch(i32(0, 0), i32(4), table, 0, 0, 4)).shape == (0, 2, 128)
+    assert pool.attn(q[:0], gb.make_page_batch(i32(0), i32(1)[:0], table[:0], 0, 0, 0)).shape == (0, 2, 128)
+    # a sequence without a page sees nothing
+    assert not pool.attn(q, gb.make_page_batch(i32(0, 1), i32(4), table[:, :0], 1, 1, 4)).any()

@@ -71,6 +71,14 @@ def test_copies_are_checked(lib, name):
         assert call(K=rows(token=0)) == inval and call(V=rows(head=0)) == inval and call(V=rows(seq=0)) == inval
 
 
+@pytest.mark.parametrize("name", ["gear_page_write", "gear_page_read"])
+def test_copies_of_no_rows(lib, name):
+    """A tensor without an entry has no address."""
+    cfg, none, one = good(), rows(data=None), rows()
+    for n_seqs, n_rows in ((0, 3), (3, 0), (0, 0)):
+        assert getattr(lib, name)(ctypes.byref(cfg), FAKE, gb.gear_page_bytes(cfg), ctypes.byref(none), ctypes.byref(one), n_seqs, n_rows, None, None) == gb.GEAR_OK
+
+
 def batch(**kw):
     b = gb.gear_page_batch(3, 7, 4, 100, 4, 1, FAKE, FAKE, FAKE)
     for k, v in kw.items():
@@ -107,6 +115,16 @@ def test_attention_is_checked(lib):
     assert call(b=batch(n_seqs=0)) == gb.GEAR_OK and call(b=batch(n_tokens=0)) == gb.GEAR_OK and call(b=batch(max_q=0)) == gb.GEAR_OK
 
 
+def test_attention_of_no_rows_and_scales_past_fp32(lib):
+    cfg, n, none = good(), gb.gear_page_bytes(good()), rows(data=None)
+
+    def call(b, q, out, scale):
+        return lib.gear_page_attn(ctypes.byref(cfg), FAKE, n, ctypes.byref(b), ctypes.byref(q), 8, scale, ctypes.byref(out), None, 0, None)
+    assert call(batch(n_tokens=0), none, none, 0.1) == gb.GEAR_OK
+    assert call(batch(n_tokens=0), none, none, 3e38) == gb.GEAR_EINVAL      # log2(e) times it is infinite
+    assert call(batch(n_tokens=0), none, none, -3e38) == gb.GEAR_EINVAL and call(batch(n_tokens=0), none, none, -2e38) == gb.GEAR_OK
+
+
 def test_a_workspace_serves_all_smaller_batches(lib):
     """The bytes grow with every bound, so what suffices for the largest batch suffices for each."""
     sizes = {}
@@ -139,3 +157,14 @@ def test_the_binding_refuses_what_the_library_cannot_see():
     for a in ((i.long(), i[:2], i.view(1, 3)), (i[:1], i[:2], i.view(1, 3)), (i[:2], i[:1], i.view(1, 3))):
         with pytest.raises(ValueError):
             gb.make_page_batch(*a, 1, 1, 1)
+
+
+def test_a_batch_of_another_gpu_is_refused(monkeypatch):
+    """The tensors of a batch are looked at when it is made; the call may come with another GPU current."""
+    cfg = gb.make_page_config(4, 16, 2, 8, 64)
+    pool, x, i = torch.zeros(gb.gear_page_bytes(cfg), dtype=torch.uint8), torch.zeros(1, 2, 128, dtype=torch.float16), torch.zeros(2, dtype=torch.int32)
+    monkeypatch.setattr(gb, "_page_device", lambda: -1)        # (where a CPU tensor's get_device() says it is)
+    b = gb.make_page_batch(i, i[:1], i.view(1, 2), 1, 1, 16)
+    monkeypatch.setattr(gb, "_page_device", lambda: 1)
+    with pytest.raises(ValueError, match="batch"):
+        gb.gear_page_attn(cfg, pool, b, x, x, 0.1, None)
