@@ -35,15 +35,13 @@ __device__ __forceinline__ void lane_extremes(uint32_t& lo, uint32_t& hi) {
 // One row piece of eight values into its place: `block` the head's Keys or Values in the page, r the row, c the lane's piece (0..15).  Every
 // lane of the wave comes here (its row's extremes are exchanged), those with `live` store.
 template <int BITS, bool BF>
-__device__ __forceinline__ void store_piece(const PageGeom& g, unsigned char* block, int r, int c, const uint4& x, bool live) {
+__device__ __forceinline__ void store_piece(const PageGeom& g, unsigned char* block, int r, int c, const uint4& v, bool live) {
   if constexpr (BITS == 16) {
-    if (live) *reinterpret_cast<uint4*>(block + (r * 16 + c) * 16) = x;
+    if (live) *reinterpret_cast<uint4*>(block + (r * 16 + c) * 16) = v;
   } else {
     constexpr float LEVELS = BITS == 8 ? 255.0f : 15.0f;
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    float f[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = to_f32<BF>(w[e >> 1] >> (16 * (e & 1)) & 0xFFFFu);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    auto value = [](uint32_t pair, int e) { return to_f32<BF>(pair >> (16 * (e & 1)) & 0xFFFFu); };
     // extremes: two values at a time as signed 16-bit integers of the same order (negative ones with their other bits turned around)
     uint32_t lo = ordered(w[0]), hi = lo;
 #pragma unroll
@@ -71,25 +69,34 @@ __device__ __forceinline__ void store_piece(const PageGeom& g, unsigned char* bl
     // the exact quotient.  The difference is exact unless the exponents lie more than 13 (bf16: 16) apart, and such a quotient is rounded
     // across a half only where it lies within 2^-17 of one.  Then the nearest integer is the sum with 1.5 * 2^23, whose last bits
     // are the code.  (Dividing: 8 x 4096 tokens of 8 heads to 4 bits 58 us.)
-    const float inv = scale > 0.0f ? recip_of_half(scale) : 0.0f, most = scale > 0.0f ? LEVELS : 0.0f;
-    if (!BF || scale >= 0x1p-100f || !(scale > 0.0f)) {
+    // A scale is off by 2^-11 (fp16) or 2^-8 (bf16) of it, more where it is denormal: only of these and of 8-bit codes in bf16 may a quotient come to more than half
+    // a step past the last code.
+    const float inv = scale > 0.0f ? recip_of_half(scale) : 0.0f;
+    float one = 1.0f;
+    GEAR_IN_VGPR(one);   // (with it, an fp16 value's conversion and the difference are one instruction, rounded once as the difference is)
+    if (scale >= (BF ? 0x1p-100f : 0x1p-14f) || !(scale > 0.0f)) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float d = __fsub_rn(f[e], mn), t = __fmul_rn(d, inv), q = __builtin_fmaf(__builtin_fmaf(-t, scale, d), inv, t);
-        code[e] = __float_as_uint(__fadd_rn(fminf(q, most), 12582912.0f));
+        const float x = value(w[e >> 1], e), d = BF ? __fsub_rn(x, mn) : __builtin_fmaf(x, one, -mn), t = __fmul_rn(d, inv), q = __builtin_fmaf(__builtin_fmaf(-t, scale, d), inv, t);
+        code[e] = __float_as_uint(__fadd_rn(BF && BITS == 8 ? fminf(q, LEVELS) : q, 12582912.0f));
       }
-    } else {   // bf16 steps whose reciprocal, or the remainder above, would leave fp32's range
+    } else {   // (bf16: the reciprocal, or the remainder above, would leave fp32's range)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) code[e] = __float_as_uint(__fadd_rn(fminf(__fdiv_rn(__fsub_rn(f[e], mn), scale), most), 12582912.0f));
+      for (int e = 0; e < 8; ++e) {
+        uint32_t pair = w[e >> 1];
+        GEAR_PIN_VGPR(pair);   // (converted in here: above, one conversion for both ways would take the place of the fused difference)
+        code[e] = __float_as_uint(__fadd_rn(fminf(__fdiv_rn(__fsub_rn(value(pair, e), mn), scale), LEVELS), 12582912.0f));
+      }
     }
     if constexpr (BITS == 8) {
       auto bytes = [](uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return GEAR_BYTE_PERM(GEAR_BYTE_PERM(d, c, 0x0C0C0400u), GEAR_BYTE_PERM(b, a, 0x0C0C0400u), 0x05040100u); };
       if (live) *reinterpret_cast<uint2*>(block + (r * 16 + c) * 8) = make_uint2(bytes(code[0], code[1], code[2], code[3]), bytes(code[4], code[5], code[6], code[7]));
     } else {
-      uint32_t y = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y |= (code[e] & 0xFu) << (4 * (e >> 1) + 16 * (e & 1));
-      if (live) *reinterpret_cast<uint32_t*>(block + (r * 16 + c) * 4) = y;
+      // (the sums' other bits, from bit 22 on, are shifted further up)
+      auto nibbles = [](uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return ((((((d << 4) + c) << 4) + b) << 4) + a); };
+      if (live)
+        *reinterpret_cast<uint32_t*>(block + (r * 16 + c) * 4) =
+            GEAR_BYTE_PERM(nibbles(code[1], code[3], code[5], code[7]), nibbles(code[0], code[2], code[4], code[6]), 0x05040100u);
     }
     if (live && ((c << 3) & ((1 << g.gshift) - 1)) == 0)
       *reinterpret_cast<uint32_t*>(block + words_at(g) + ((((c << 3) >> g.gshift) << g.shift) + r) * 4) = sz;
@@ -134,22 +141,22 @@ __global__ __launch_bounds__(COPY_THREADS) void page_copy_kernel(PageCopy a) {
   const PageGeom& g = a.geom;
   const int h = (int)(blockIdx.x % (unsigned)g.H), c = threadIdx.x & 15;
   const uint32_t t = blockIdx.x / (unsigned)g.H * (COPY_THREADS / 16) + (threadIdx.x >> 4), s = t / (uint32_t)a.n_rows, r = t - s * (uint32_t)a.n_rows;
-  const int64_t slot = (int64_t)t < a.total ? a.slots[t] : -1;
+  unsigned char* const kp = a.k.data + 2 * (s * a.k.seq + r * a.k.token + h * a.k.head + 8 * c);
+  unsigned char* const vp = a.v.data + 2 * (s * a.v.seq + r * a.v.token + h * a.v.head + 8 * c);
+  uint4 k = make_uint4(0, 0, 0, 0), v = k;
+  const bool there = (int64_t)t < a.total;
+  if (WRITE && there) {   // (on their way with the slot, a row that is skipped too: 42.5 -> 39.6 us)
+    k = *reinterpret_cast<const uint4*>(kp);
+    v = *reinterpret_cast<const uint4*>(vp);
+  }
+  const int64_t slot = there ? a.slots[t] : -1;
   const bool live = slot >= 0 && slot < (int64_t)g.n_pages << g.shift;   // the same for the 16 lanes of a row
   const int64_t at = live ? slot : 0;
   const unsigned char* const keys = block_of(g, (int)(at >> g.shift), h, 0);
   const int row = (int)(at & page_mask(g));
-  unsigned char* const kp = a.k.data + 2 * (s * a.k.seq + r * a.k.token + h * a.k.head + 8 * c);
-  unsigned char* const vp = a.v.data + 2 * (s * a.v.seq + r * a.v.token + h * a.v.head + 8 * c);
-  uint4 k = make_uint4(0, 0, 0, 0), v = k;
-  if (live) {
-    if constexpr (WRITE) {
-      k = *reinterpret_cast<const uint4*>(kp);
-      v = *reinterpret_cast<const uint4*>(vp);
-    } else {
-      if (a.k.data) k = load_piece<BITS, BF>(g, keys, row, c);
-      if (a.v.data) v = load_piece<BITS, BF>(g, keys + g.block_bytes, row, c);
-    }
+  if (!WRITE && live) {
+    if (a.k.data) k = load_piece<BITS, BF>(g, keys, row, c);
+    if (a.v.data) v = load_piece<BITS, BF>(g, keys + g.block_bytes, row, c);
   }
   if constexpr (WRITE) {
     unsigned char* block = const_cast<unsigned char*>(keys);
