@@ -154,7 +154,8 @@ int copy_rows(const gear_page_config* cfg, const void* pool, size_t pool_bytes, 
   if (V && (rc = check_rows(V, n_seqs, n_rows, cfg->H_kv, !write))) return rc;
   if (!slots) return GEAR_EINVAL;
   if (misaligned(slots, 8)) return GEAR_EALIGN;
-  if (total > INT_MOST - 4096 || (total + 15) / 16 * cfg->H_kv > THREADS_MOST / 256) return GEAR_ECAPACITY;
+  const int64_t chunks = n_rows == 1 ? ((int64_t)n_seqs + 15) / 16 : (int64_t)n_seqs * (((int64_t)n_rows + 15) / 16);   // of 16 rows, a block for each head, at most
+  if (total > INT_MOST - 4096 || chunks * cfg->H_kv > THREADS_MOST / 256) return GEAR_ECAPACITY;
   return launch_page_copy(g, cfg->bits, cfg->dtype == GEAR_BF16, write, view_of(K), view_of(V), slots, n_seqs, n_rows,
                           static_cast<hipStream_t>(stream)) == hipSuccess ? GEAR_OK : GEAR_EHIP;
 }

@@ -12,7 +12,7 @@ struct PageCopy {
   RowView k, v;
   const int64_t* slots;
   int32_t n_rows;     // rows per sequence
-  int64_t total;      // rows of all sequences, below 2^31
+  int32_t chunks;     // blocks per sequence and head
 };
 
 typedef short i16x2_t __attribute__((ext_vector_type(2)));
@@ -27,10 +27,7 @@ __device__ __forceinline__ uint32_t ordered(uint32_t x) {
   return x ^ (__builtin_bit_cast(uint32_t, __builtin_bit_cast(i16x2_t, x) >> 15) & 0x7FFF7FFFu);
 }
 template <int CTRL>
-__device__ __forceinline__ void lane_extremes(uint32_t& lo, uint32_t& hi) {
-  lo = min_i16x2(lo, dpp_u<CTRL>(lo));
-  hi = max_i16x2(hi, dpp_u<CTRL>(hi));
-}
+__device__ __forceinline__ uint32_t lanes_max(uint32_t x) { return max_i16x2(x, dpp_u<CTRL>(x)); }
 
 // One row piece of eight values into its place: `block` the head's Keys or Values in the page, r the row, c the lane's piece (0..15).  Every
 // lane of the wave comes here (its row's extremes are exchanged), those with `live` store.
@@ -50,14 +47,16 @@ __device__ __forceinline__ void store_piece(const PageGeom& g, unsigned char* bl
       lo = min_i16x2(lo, k);
       hi = max_i16x2(hi, k);
     }
-    lane_extremes<DPP_XOR1>(lo, hi);
-    lane_extremes<DPP_XOR2>(lo, hi);
-    if (g.gshift > 5) lane_extremes<DPP_HALF_MIRROR>(lo, hi);
-    if (g.gshift > 6) lane_extremes<DPP_MIRROR>(lo, hi);
     lo = min_i16x2(lo, lo >> 16 | lo << 16);
     hi = max_i16x2(hi, hi >> 16 | hi << 16);
-    const uint32_t zero = ordered(lo) & 0xFFFFu;
-    const float mn = to_f32<BF>(zero), mx = to_f32<BF>(ordered(hi) & 0xFFFFu);
+    uint32_t ext = (hi & 0xFFFFu) | (~lo & 0xFFFF0000u);   // (the greatest complement is that of the least)
+    ext = lanes_max<DPP_XOR1>(ext);
+    ext = lanes_max<DPP_XOR2>(ext);
+    if (g.gshift > 5) ext = lanes_max<DPP_HALF_MIRROR>(ext);
+    if (g.gshift > 6) ext = lanes_max<DPP_MIRROR>(ext);
+    ext = ordered(ext ^ 0xFFFF0000u);
+    const uint32_t zero = ext >> 16;
+    const float mn = to_f32<BF>(zero), mx = to_f32<BF>(ext & 0xFFFFu);
     // (a quotient as below; 1 / 255 and 1 / 15 are constants)
     const float range = __fsub_rn(mx, mn), by = __fmul_rn(range, 1.0f / LEVELS);
     float s32 = __builtin_fmaf(__builtin_fmaf(-by, LEVELS, range), 1.0f / LEVELS, by);
@@ -116,14 +115,14 @@ __device__ __forceinline__ uint4 load_piece(const PageGeom& g, const unsigned ch
   }
 }
 
-constexpr int COPY_THREADS = 256;
+constexpr int COPY_THREADS = 256, COPY_ROWS = COPY_THREADS / 16;
 #ifndef GEAR_PAGE_PAST_CACHES   // (the CPU stand-in lowers it)
 #define GEAR_PAGE_PAST_CACHES (64ll << 20)
 #endif
 constexpr int64_t PAST_CACHES = GEAR_PAGE_PAST_CACHES;   // bytes of both tensors
 
 // What is brought back once and is larger than the caches is stored past them (7 x 1777 tokens of 40 heads, 255 MB: 79 -> 47 us;
-// 16 x 4096 of 32, 1.07 GB: 314 -> 288).
+// 16 x 4096 of 32, 1.07 GB: 314 -> 289).
 template <bool PAST>
 __device__ __forceinline__ void store16(unsigned char* p, const uint4& v) {
 #ifdef GEAR_NO_NONTEMPORAL
@@ -134,22 +133,24 @@ __device__ __forceinline__ void store16(unsigned char* p, const uint4& v) {
 #endif
 }
 
-// grid: (head, 16 rows), heads next to each other.  A row per 16 lanes: with two or four, whose loads are requested together, the writes took 4 and 12 %
-// longer (the chip's waves have enough on their way).
+// grid: (head, 16 rows of one sequence), heads next to each other: all but a lane's row and piece is known to the block, whose scalar unit
+// works it out (with a sequence per lane, the same 38.2, not 35.8).  A row per 16 lanes: with two or four, whose loads are
+// requested together, the writes took 4 and 12 % longer.
 template <int BITS, bool BF, bool WRITE, bool PAST>
 __global__ __launch_bounds__(COPY_THREADS) void page_copy_kernel(PageCopy a) {
   const PageGeom& g = a.geom;
-  const int h = (int)(blockIdx.x % (unsigned)g.H), c = threadIdx.x & 15;
-  const uint32_t t = blockIdx.x / (unsigned)g.H * (COPY_THREADS / 16) + (threadIdx.x >> 4), s = t / (uint32_t)a.n_rows, r = t - s * (uint32_t)a.n_rows;
-  unsigned char* const kp = a.k.data + 2 * (s * a.k.seq + r * a.k.token + h * a.k.head + 8 * c);
-  unsigned char* const vp = a.v.data + 2 * (s * a.v.seq + r * a.v.token + h * a.v.head + 8 * c);
+  const unsigned bid = blockIdx.x, rest = bid / (unsigned)g.H, s = rest / (unsigned)a.chunks;
+  const int h = (int)(bid - rest * (unsigned)g.H), c = threadIdx.x & 15, in_chunk = threadIdx.x >> 4;
+  const int first = (int)(rest - s * (unsigned)a.chunks) * COPY_ROWS;
+  unsigned char* const kp = a.k.data + 2 * ((int64_t)s * a.k.seq + (int64_t)first * a.k.token + h * a.k.head) + 2 * (in_chunk * a.k.token + 8 * c);
+  unsigned char* const vp = a.v.data + 2 * ((int64_t)s * a.v.seq + (int64_t)first * a.v.token + h * a.v.head) + 2 * (in_chunk * a.v.token + 8 * c);
   uint4 k = make_uint4(0, 0, 0, 0), v = k;
-  const bool there = (int64_t)t < a.total;
-  if (WRITE && there) {   // (on their way with the slot, a row that is skipped too: 42.5 -> 39.6 us)
+  const bool there = first + in_chunk < a.n_rows;
+  if (WRITE && there) {   // (on their way with the slot, a row that is skipped too: 8 x 4096 tokens of 8 heads to 4 bits 42.5 -> 39.6 us)
     k = *reinterpret_cast<const uint4*>(kp);
     v = *reinterpret_cast<const uint4*>(vp);
   }
-  const int64_t slot = there ? a.slots[t] : -1;
+  const int64_t slot = there ? a.slots[(int64_t)s * a.n_rows + first + in_chunk] : -1;
   const bool live = slot >= 0 && slot < (int64_t)g.n_pages << g.shift;   // the same for the 16 lanes of a row
   const int64_t at = live ? slot : 0;
   const unsigned char* const keys = block_of(g, (int)(at >> g.shift), h, 0);
@@ -163,29 +164,41 @@ __global__ __launch_bounds__(COPY_THREADS) void page_copy_kernel(PageCopy a) {
     store_piece<BITS, BF>(g, block, row, c, k, live);
     store_piece<BITS, BF>(g, block + g.block_bytes, row, c, v, live);
   } else if (live) {
+    if (a.v.data) store16<PAST>(vp, v);   // (the later request first, so that the stores leave together: 16 x 4096 tokens 289 us, not 300)
     if (a.k.data) store16<PAST>(kp, k);
-    if (a.v.data) store16<PAST>(vp, v);
   }
 }
 
 template <int BITS, bool BF, bool WRITE>
-static hipError_t launch_copy(const PageCopy& a, hipStream_t st) {
-  const int64_t per = COPY_THREADS / 16, blocks = (a.total + per - 1) / per * a.geom.H;
-  if (!WRITE && a.total * a.geom.H * (4 * D) >= PAST_CACHES)
+static hipError_t launch_copy(const PageCopy& a, int n_seqs, hipStream_t st) {
+  const int64_t blocks = (int64_t)n_seqs * a.chunks * a.geom.H;
+  if (!WRITE && (int64_t)n_seqs * a.n_rows * a.geom.H * (4 * D) >= PAST_CACHES)
     hipLaunchKernelGGL((page_copy_kernel<BITS, BF, WRITE, !WRITE>), dim3((unsigned)blocks), dim3(COPY_THREADS), 0, st, a);
   else
     hipLaunchKernelGGL((page_copy_kernel<BITS, BF, WRITE, false>), dim3((unsigned)blocks), dim3(COPY_THREADS), 0, st, a);
   return hipGetLastError();
 }
 
+static bool one_run(const RowView& r, int64_t n_rows) { return !r.data || r.seq == n_rows * r.token; }
+
 hipError_t launch_page_copy(const PageGeom& g, int bits, bool bf, bool write, const RowView& k, const RowView& v, const int64_t* slots,
                             int n_seqs, int n_rows, hipStream_t st) {
-  const PageCopy a{g, k, v, slots, n_rows, (int64_t)n_seqs * n_rows};
+  PageCopy a{g, k, v, slots, n_rows, 1};
+  if (n_rows == 1) {   // single tokens, and sequences that follow one another: the rows of one
+    a.k.token = k.seq;
+    a.v.token = v.seq;
+    a.n_rows = n_seqs;
+    n_seqs = 1;
+  } else if (one_run(k, n_rows) && one_run(v, n_rows)) {
+    a.n_rows = n_seqs * n_rows;
+    n_seqs = 1;
+  }
+  a.chunks = (a.n_rows + COPY_ROWS - 1) / COPY_ROWS;
 #define GEAR_PAGE_COPY(B)                                                                     \
-  return bf ? (write ? launch_copy<B, true, true>(a, st) : launch_copy<B, true, false>(a, st)) \
-            : (write ? launch_copy<B, false, true>(a, st) : launch_copy<B, false, false>(a, st))
+  return bf ? (write ? launch_copy<B, true, true>(a, n_seqs, st) : launch_copy<B, true, false>(a, n_seqs, st)) \
+            : (write ? launch_copy<B, false, true>(a, n_seqs, st) : launch_copy<B, false, false>(a, n_seqs, st))
   if (bits == 16) {   // (copied as they are: the type does not matter)
-    return write ? launch_copy<16, false, true>(a, st) : launch_copy<16, false, false>(a, st);
+    return write ? launch_copy<16, false, true>(a, n_seqs, st) : launch_copy<16, false, false>(a, n_seqs, st);
   }
   if (bits == 8) GEAR_PAGE_COPY(8);
   GEAR_PAGE_COPY(4);
