@@ -408,3 +408,35 @@ def test_calls_of_no_rows():
     assert pool.attn(q[:0], gb.make_page_batch(i32(0), i32(1)[:0], table[:0], 0, 0, 0)).shape == (0, 2, 128)
     # a sequence without a page sees nothing
     assert not pool.attn(q, gb.make_page_batch(i32(0, 1), i32(4), table[:, :0], 1, 1, 4)).any()
+
+
+@pytest.mark.parametrize("form", [FORMS[0], FORMS[3], FORMS[6]], ids=FORM_IDS)
+@pytest.mark.parametrize("S,n", [(20, 1), (3, 5), (2, 16), (2, 33)])
+@pytest.mark.parametrize("order", ["rows", "heads", "both", "gaps", "expanded"])
+def test_orders_of_rows(order, S, n, form):
+    """Sequences that follow one another in memory and such that do not, Keys and Values of one order or of two; one row for all sequences."""
+    dtype, bits, group = form
+    H, page = 3, 16
+    gen = torch.Generator().manual_seed(S * n + bits)
+    width = -(-n // page)
+    pool = gb.PagePool(gb.make_page_config(S * width, page, H, bits, group, dtype), DEV)
+    x = [torch.randn((S, n, H, 128), generator=gen).to(dtype) for _ in range(2)]
+    if order == "expanded":
+        x = [t[:1].expand(S, n, H, 128) for t in x]
+
+    def placed(t, heads, gaps):
+        t = t.to(DEV) if order != "expanded" else t[:1].to(DEV).expand(S, n, H, 128)
+        if heads:
+            return t.transpose(1, 2).contiguous().transpose(1, 2)
+        if gaps:
+            wide = torch.zeros((S + 1, n + 2, H, 128 + 8), dtype=dtype, device=DEV)
+            wide[:S, :n, :, :128] = t
+            return wide[:S, :n, :, :128]
+        return t
+    K, V = placed(x[0], order in ("heads", "both"), order == "gaps"), placed(x[1], order == "heads", order == "gaps")
+    pos = torch.arange(n)
+    slots = (torch.randperm(S * width, generator=gen).view(S, width)[:, pos // page] * page + pos % page).to(DEV)
+    pool.write(K, V, slots)
+    for heads_first in (False, True):
+        for got, t in zip(pool.read(slots, heads_first), x):
+            assert bits_equal(got.transpose(1, 2) if heads_first else got, pg.expected(t.contiguous(), bits, group, dtype))
