@@ -213,7 +213,7 @@ struct PageAttn {
   int32_t tiles;     // column tiles of page_attn_many_kernel, at most
 };
 constexpr int KEY_STEP = 32, MANY_COLS = 128, MANY_KEYS = 64;
-constexpr int FEW_PART = 512, MANY_PART = 128;   // tokens of a part, at least
+constexpr int FEW_PART = 256, MANY_PART = 128;   // tokens of a part, at least (of few columns: one step of a block's waves)
 
 // The key axis of `keys` tokens in at most n_split equal parts of about `least` tokens and more, multiples of `unit`: tokens of a part, and how many
 // there are (at least one).
