@@ -19,14 +19,15 @@ __global__ __launch_bounds__(64 * MERGE_WAVES) void page_merge_few_kernel(PageAt
   GEAR_DYN_LDS(lds);
   const PageGeom& g = a.geom;
   const int bid = (int)blockIdx.x, col = bid % a.few_cols, rest = bid / a.few_cols, head = rest % g.H, s = rest / g.H;
+  const int lane = lane_id(), wave = (int)(threadIdx.x >> 6);
+  const int64_t rec = (((int64_t)s * g.H + head) * a.few_cols + col) * a.n_split;
+  FirstRecords first = first_records<MERGE_WAVES>(a, rec, wave, lane);
   const SeqSpan sp = seq_span(a, s);
   const int cols = sp.nq * a.gq;
   if (sp.nq <= 0 || sp.nq > a.few || cols > a.few || col >= cols) return;
   const Parts parts = parts_of(sp.kv, a.n_split, a.least, KEY_STEP);
   if (parts.count <= 1) return;
-  const int lane = lane_id(), wave = (int)(threadIdx.x >> 6);
-  const int64_t rec = (((int64_t)s * g.H + head) * a.few_cols + col) * a.n_split;
-  const Merged x = merge_records<MERGE_WAVES>(a, rec, parts.count, wave, lane, reinterpret_cast<float*>(lds));
+  const Merged x = merge_records<MERGE_WAVES>(first, a, rec, parts.count, wave, lane, reinterpret_cast<float*>(lds));
   if (wave == 0) store_merged(a, x, sp.q0 + col / a.gq, head * a.gq + col % a.gq, lane, bf);
 }
 

@@ -20,12 +20,14 @@ __global__ __launch_bounds__(256) void page_merge_many_kernel(PageAttn a, int bf
   const int lane = lane_id(), Hq = g.H * a.gq, wave = (int)(threadIdx.x >> 6), mine = WAVES == 1 ? 0 : wave;
   const int64_t id = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
   const int token = (int)(id / Hq), jq = (int)(id - (int64_t)token * Hq), head = jq / a.gq;
+  if (token >= a.n_tokens) return;
+  FirstRecords first = first_records<WAVES>(a, id * a.n_split, mine, lane);
   int s = -1;
   for (int base = 0; base < a.n_seqs; base += 64) {
     const int i = base + lane;
     s += __popcll(__ballot(i < a.n_seqs && a.q_start[i] <= token));
   }
-  if (s < 0 || token >= a.n_tokens) return;
+  if (s < 0) return;
   s = GEAR_WAVE_UNIFORM(s);
   const SeqSpan sp = seq_span(a, s);
   const int row = token - sp.q0, cols = sp.nq * a.gq;
@@ -33,7 +35,7 @@ __global__ __launch_bounds__(256) void page_merge_many_kernel(PageAttn a, int bf
   const int col = row * a.gq + (jq - head * a.gq), last = min(col / MANY_COLS * MANY_COLS + MANY_COLS, cols) - 1;
   const int count = parts_of(row_sees(a, sp, last / a.gq), a.n_split, a.least, MANY_KEYS).count;
   if (count <= 1) return;
-  const Merged x = merge_records<WAVES>(a, id * a.n_split, count, mine, lane, reinterpret_cast<float*>(lds));
+  const Merged x = merge_records<WAVES>(first, a, id * a.n_split, count, mine, lane, reinterpret_cast<float*>(lds));
   if (mine == 0) store_merged(a, x, token, jq, lane, bf);
 }
 

@@ -9,32 +9,48 @@ constexpr int MERGE_WAVES = 4, MERGE_LDS = MERGE_WAVES * 3 * 64 * 4;
 struct Merged {   // a lane's two channels, and the sum of the weights
   float sum, x, y;
 };
-// WAVES waves take the records of `count` parts from `rec` on in turn, eight of each on their way at a time; wave 0 has the result.  lds: [wave][3][lane].
-template <int WAVES>
-__device__ __forceinline__ Merged merge_records(const PageAttn& a, int64_t rec, int count, int wave, int lane, float* lds) {
+// Eight records of a wave on their way.
+struct Records {
   float2 ml[8], v[8];
-  auto request = [&](int i0) {
+};
+template <int WAVES>
+__device__ __forceinline__ void request_records(Records& r, const PageAttn& a, int64_t rec, int i0, int lane) {   // in the row, whatever lies behind its parts
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int64_t i = rec + min(i0 + WAVES * u, count - 1);
-      ml[u] = a.rec_ml[i];
-      v[u] = *reinterpret_cast<const float2*>(a.rec_o + i * D + 2 * lane);
-    }
-  };
-  request(wave);   // (with the maxima, which each wave looks through by itself)
-  float top = a.rec_ml[rec + min(lane, count - 1)].x;
+  for (int u = 0; u < 8; ++u) {
+    const int64_t i = rec + min(i0 + WAVES * u, a.n_split - 1);
+    r.ml[u] = a.rec_ml[i];
+    r.v[u] = *reinterpret_cast<const float2*>(a.rec_o + i * D + 2 * lane);
+  }
+}
+// What a wave asks for before it knows how many parts there are (the lengths are on their way then, too): its first records, and a maximum per lane.
+struct FirstRecords {
+  Records r;
+  float top;
+};
+template <int WAVES>
+__device__ __forceinline__ FirstRecords first_records(const PageAttn& a, int64_t rec, int wave, int lane) {
+  FirstRecords f;
+  request_records<WAVES>(f.r, a, rec, wave, lane);
+  f.top = a.rec_ml[rec + min(lane, a.n_split - 1)].x;
+  return f;
+}
+// WAVES waves take the records of `count` parts from `rec` on in turn; wave 0 has the result.  lds: [wave][3][lane].
+template <int WAVES>
+__device__ __forceinline__ Merged merge_records(FirstRecords& f, const PageAttn& a, int64_t rec, int count, int wave, int lane, float* lds) {
+  float top = lane < count ? f.top : -INFINITY;   // (of all parts: each wave looks through them by itself)
   for (int i = lane + 64; i < count; i += 64) top = fmaxf(top, a.rec_ml[rec + i].x);
   top = wave_max(top);
   const float from = top == -INFINITY ? 0.0f : top;
   Merged m{0.0f, 0.0f, 0.0f};
   for (int i0 = wave; i0 < count; i0 += WAVES * 8) {
-    if (i0 != wave) request(i0);
+    if (i0 != wave) request_records<WAVES>(f.r, a, rec, i0, lane);
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const float by = i0 + WAVES * u < count ? GEAR_EXP2(ml[u].x - from) : 0.0f;
-      m.sum += ml[u].y * by;
-      m.x += v[u].x * by;
-      m.y += v[u].y * by;
+      const bool there = i0 + WAVES * u < count;
+      const float by = there ? GEAR_EXP2(f.r.ml[u].x - from) : 0.0f;
+      m.sum += there ? f.r.ml[u].y * by : 0.0f;
+      m.x += there ? f.r.v[u].x * by : 0.0f;
+      m.y += there ? f.r.v[u].y * by : 0.0f;
     }
   }
   if constexpr (WAVES > 1) {

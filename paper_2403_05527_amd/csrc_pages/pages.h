@@ -252,12 +252,14 @@ struct PageRow {
 __device__ __forceinline__ PageRow page_row(const PageAttn& a, int s, int end) {
   return PageRow{a.table + (int64_t)s * a.width, -64, 0, a.geom.n_pages, a.geom.shift, end, 0ull};
 }
-__device__ __forceinline__ void load_entries(PageRow& r, int i) {   // from entry i on, which is one of a key before `end`; behind the last: that one
+__device__ __forceinline__ void hold_entries(PageRow& r, int i, int32_t entry) {   // the lane's entry, i + its number
   r.base = i;
-  const int at = i + lane_id(), last = (r.end - 1) >> r.shift;
-  const int p = r.table[at <= last ? at : last];
-  r.held = p >= 0 && p < r.n_pages ? p : -1;
+  r.held = entry >= 0 && entry < r.n_pages ? entry : -1;
   r.valid = __ballot(r.held >= 0);
+}
+__device__ __forceinline__ void load_entries(PageRow& r, int i) {   // from entry i on, which is one of a key before `end`; behind the last: that one
+  const int at = i + lane_id(), last = (r.end - 1) >> r.shift;
+  hold_entries(r, i, r.table[at <= last ? at : last]);
 }
 // The page of a key (the same in all lanes of the wave); -1: none.  Keys are asked for in ascending order.
 __device__ __forceinline__ int page_of(PageRow& r, int key) {
