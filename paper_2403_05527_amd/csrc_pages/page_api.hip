@@ -17,11 +17,11 @@ constexpr int FEW_BLOCKS_MOST = FEW_SLOTS * 3 / 2, MANY_BLOCKS_MOST = MANY_SLOTS
 // The number of equal parts of the key axis that a model finds the fastest, in ns: `blocks` of them undivided on `slots` places, each taking `once` and 2 us
 // per `step` tokens, begun or whole; all together no less than `bytes` (the memory's share); with more than one part, a merge whose records (`records` bytes
 // per part) are written and read at 5 TB/s.  A quarter of the lesser of the two bounds is added: blocks of unequal length.
-// crowded: what a block's time is multiplied by where there are more than CUs.
+// crowded: what a block's time is multiplied by where there are more than CUs (the last to end shares its CU); `merges`: the blocks of the merge, 2.2 ns each.
 // filled: parts have a length, not a number, so sequences shorter than max_kv make fewer; but no more than 86 % of the slots count, since blocks that end at once
 // leave the XCDs unevenly filled (504 parts on 512 slots: the last dozen began when the first had ended).
 static int best_parts(int64_t blocks, double filled, int slots, int most_blocks, int max_kv, int least_part, double once, int step, double crowded, double bytes,
-                      double records) {
+                      double records, double merges) {
   const int64_t by_blocks = blocks > 0 ? most_blocks / blocks : 1;
   const int by_keys = max_kv / least_part, most = (int)(by_blocks < by_keys ? by_blocks : by_keys);
   int best = 1;
@@ -30,7 +30,7 @@ static int best_parts(int64_t blocks, double filled, int slots, int most_blocks,
     const int64_t len = ((int64_t)max_kv + n - 1) / n;
     const double block = (once + 2000.0 * (double)((len + step - 1) / step)) * (blocks * n > GEAR_PAGE_CUS ? crowded : 1.0);
     const double time = std::ceil((n > 1 ? filled / 0.86 : 1.0) * (double)(blocks * n) / slots) * block;
-    const double t = (time > bytes ? time + 0.25 * bytes : bytes + 0.25 * time) + (n > 1 ? 4000.0 + 20.0 * n + records * n * 2.0 / 5000.0 : 0.0);
+    const double t = (time > bytes ? time + 0.25 * bytes : bytes + 0.25 * time) + (n > 1 ? 4000.0 + 20.0 * n + 2.2 * merges + records * n * 2.0 / 5000.0 : 0.0);
     if (n == 1 || t < least) {
       best = n;
       least = t;
@@ -50,14 +50,24 @@ PagePlan page_plan(int H, int gq, int n_seqs, int n_tokens, int max_q, int max_k
   p.few_limit = !p.few ? 0 : all_few ? (int)cols : gq <= 16 ? 16 : FEW_COLS_MOST;
   p.few_tiles = p.few_limit <= 16 ? 1 : 2;
   p.few_split = p.many_split = 1;
+  // Both in one launch (page_mixed.hip), but where the few columns' bytes take most of the time, and long: there their blocks are better off with eight waves
+  // and the chip to themselves.  Estimates in us, at 6 TB/s and 1 PFLOP/s, from the bounds alone.  (One launch and two: 33 sequences of up to 4000 tokens,
+  // three of them chunks of up to 700, 110 and 150 us; 20 of up to 1000 tokens, one chunk of 100, 34 and 50; 10 of up to 5908 tokens of 32
+  // heads at 16 bits, two chunks of 415, 231 and 194.)
+  const double few_us = (double)n_seqs * H * max_kv * bytes_per_key / 6e6, many_us = (double)n_tokens * H * gq * max_kv * 512.0 / 1e9;
+  p.one_launch = p.few && p.many && !(few_us > 100.0 && few_us > 2.0 * many_us);
   const double filled = n_seqs >= 4 ? 0.75 : 1.0;
   if (p.few) {
-    // A block of eight waves: 4 us (its launch, the first loads, the joining of its waves) and 2 us per step of its waves, 256 tokens.  In graphs: 1 x 8 heads x
-    // 8192 tokens at 8 bits 10.7 us in 32 parts, 12.4 in 16, 16.0 in 8; four rows of 5 sequences of 3000 tokens 16.1 in 6, 240 blocks, 18.0 in 8 and 17.6 in 11; 1 x 8
-    // heads x 32768 at 4 bits 21.2 in 96, 16.7 in 64, 18.2 in 32; 33 sequences of 600 to 4000 tokens, 264 blocks: 46 undivided, 41 and 15 of merging in three parts.
+    // A block of eight waves: 4 us (its launch, the first loads, the joining of its waves) and 2 us per step of its waves, 256 tokens; more blocks than CUs take a
+    // third longer.  In graphs: 1 x 8 heads x 8192 tokens at 8 bits 10.2 us in 32 parts, 12.4 in 16, 16.0 in 8; x 32768 at 4 bits 15.9 in 32, 19.0 in 43, 18.0 in
+    // 55; four rows of 5 sequences of 3000 tokens 15.0 in 6, 240 blocks, 18.0 in 8 and 17.6 in 11.  33 sequences of 600 to 4000 tokens, 264 blocks: 46 undivided, 41
+    // and 15 of merging in three parts.
     const int64_t blocks = (int64_t)n_seqs * H;
-    p.few_split = best_parts(blocks, filled, p.few_tiles == 1 ? FEW_SLOTS : FEW_SLOTS / 2, FEW_BLOCKS_MOST, max_kv, FEW_PART, 4000.0, FEW_PART, 1.35,
-                             (double)blocks * max_kv * bytes_per_key / 6000.0, (double)blocks * p.few_limit * RECORD_BYTES);
+    // In one launch with blocks of many columns they have four waves, a step is half as long, and nobody waits for them before the others' operations are done
+    // (6 sequences of up to 3000 tokens, 32 heads, one of them a chunk of up to 200: 58 us as if alone, 48 so).
+    const double bytes_ns = 1000.0 * few_us + (p.one_launch ? 1000.0 * many_us : 0.0), records = (double)blocks * p.few_limit;
+    p.few_split = best_parts(blocks, filled, p.few_tiles == 1 ? FEW_SLOTS : FEW_SLOTS / 2, FEW_BLOCKS_MOST, max_kv, FEW_PART, 4000.0, p.one_launch ? FEW_PART / 2 : FEW_PART,
+                             p.one_launch ? 1.0 : 1.35, bytes_ns, records * RECORD_BYTES, records);
     if (p.few_split > 1) p.few_rows = (int64_t)n_seqs * H * p.few_limit;
   }
   if (p.many) {
@@ -65,16 +75,10 @@ PagePlan page_plan(int H, int gq, int n_seqs, int n_tokens, int max_q, int max_k
     // alone; three chunks of 483 to 566 behind up to 2900, 416 blocks: 100 us undivided, 140 in two parts.
     const int64_t tiles = uniform ? (cols + MANY_COLS - 1) / MANY_COLS * n_seqs : ((int64_t)n_tokens * gq + MANY_COLS - 1) / MANY_COLS;
     const int64_t rows = (int64_t)n_tokens * H * gq;
-    p.many_split = best_parts(tiles * H, filled, MANY_SLOTS, MANY_BLOCKS_MOST, max_kv, MANY_PART, 6000.0, MANY_KEYS, 1.0, 0.0, (double)rows * RECORD_BYTES);
+    p.many_split = best_parts(tiles * H, filled, MANY_SLOTS, MANY_BLOCKS_MOST, max_kv, MANY_PART, 6000.0, MANY_KEYS, 1.0, 0.0, (double)rows * RECORD_BYTES, 0.0);
     p.many_least = max_kv / p.many_split > MANY_PART ? max_kv / p.many_split : MANY_PART;
     if (p.many_split > 1) p.many_rows = (int64_t)n_tokens * H * gq;
   }
-  // Both in one launch (page_mixed.hip), but where the few columns' bytes take most of the time, and long: there their blocks are better off with eight waves
-  // and the chip to themselves.  Estimates in us, at 6 TB/s and 1 PFLOP/s, from the bounds alone.  (One launch and two: 33 sequences of up to 4000 tokens,
-  // three of them chunks of up to 700, 110 and 150 us; 20 of up to 1000 tokens, one chunk of 100, 34 and 50; 10 of up to 5908 tokens of 32
-  // heads at 16 bits, two chunks of 415, 231 and 194.)
-  const double few_us = (double)n_seqs * H * max_kv * bytes_per_key / 6e6, many_us = (double)n_tokens * H * gq * max_kv * 512.0 / 1e9;
-  p.one_launch = p.few && p.many && !(few_us > 100.0 && few_us > 2.0 * many_us);
   return p;
 }
 
