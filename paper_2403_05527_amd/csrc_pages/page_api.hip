@@ -250,18 +250,20 @@ int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_by
   a.few = p.few_limit;
   a.few_cols = p.few_limit;
   a.tiles = (int32_t)tiles;
-  float* rec = static_cast<float*>(workspace);
+  // the sums of both kinds, 512 bytes a record (they are stored 16 bytes at a time), then the (maximum, sum) pairs
+  float* const sums = static_cast<float*>(workspace);
+  float2* const pairs = reinterpret_cast<float2*>(sums + (many_recs + few_recs) * D);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   const bool bf = cfg->dtype == GEAR_BF16;
   PageAttn m = a, f = a;
   m.n_split = p.many_split;
   m.least = p.many_least;
-  m.rec_o = rec;
-  m.rec_ml = reinterpret_cast<float2*>(rec + many_recs * D);
+  m.rec_o = sums;
+  m.rec_ml = pairs;
   f.n_split = p.few_split;
   f.least = FEW_PART;
-  f.rec_o = rec + many_recs * (D + 2);
-  f.rec_ml = reinterpret_cast<float2*>(f.rec_o + few_recs * D);
+  f.rec_o = sums + many_recs * D;
+  f.rec_ml = pairs + many_recs;
   if (p.one_launch) return launch_page_mixed(m, f, cfg->bits, bf, p.few_tiles, st) == hipSuccess ? GEAR_OK : GEAR_EHIP;
   if (p.many && launch_page_many(m, cfg->bits, bf, st) != hipSuccess) return GEAR_EHIP;
   if (p.few && launch_page_few(f, cfg->bits, bf, p.few_tiles, st) != hipSuccess) return GEAR_EHIP;

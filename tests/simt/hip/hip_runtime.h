@@ -28,7 +28,20 @@ using std::max;
 struct dim3 { unsigned x, y, z; dim3(unsigned a = 1, unsigned b = 1, unsigned c = 1) : x(a), y(b), z(c) {} };
 struct uint2 { uint32_t x, y; };
 struct alignas(16) uint4 { uint32_t x, y, z, w; };
+#ifdef SIMT_ALIGNED_STORES   // (the alignment sanitizer does not look at assignments of structures)
+struct alignas(16) float4 {
+  float x, y, z, w;
+  float4& operator=(const float4& v) {
+    uintptr_t at = reinterpret_cast<uintptr_t>(this);
+    asm volatile("" : "+r"(at));   // (the compiler takes the type's word for it)
+    if (at % 16) { fprintf(stderr, "runtime error: 16 bytes stored at %p\n", (void*)at); abort(); }
+    x = v.x; y = v.y; z = v.z; w = v.w;
+    return *this;
+  }
+};
+#else
 struct alignas(16) float4 { float x, y, z, w; };
+#endif
 struct float2 { float x, y; };
 struct alignas(16) double2 { double x, y; };
 static inline double2 make_double2(double x, double y) { return double2{x, y}; }
@@ -341,7 +354,9 @@ inline void launch(const void* kernel, const char* name, dim3 grid, dim3 block, 
 #define GEAR_MERGE_16 3
 #define GEAR_MERGE_32 4
 #endif
+#ifndef GEAR_PAGE_CUS
 #define GEAR_PAGE_CUS 4           // the paged cache's attention in parts
+#endif
 #ifndef GEAR_BLOCK_SLOTS
 #define GEAR_BLOCK_SLOTS 16       // and strips of two tiles and more
 #endif

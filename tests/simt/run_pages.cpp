@@ -75,6 +75,9 @@ int main(int, char** argv) {
     const gear_page_rows qr{q.p, 0, (int64_t)H_q * 128, 128}, orow{out.p, 0, (int64_t)H_q * 128, 128};
     CHECK(gear_page_attn(&c, pool.p, pool.n, &b, &qr, H_q, scale, &orow, ws.p, ws.n, nullptr));
     out.save("out.bin");
+    size_t words = 0;   // a record: 130 words, none of which is the filling
+    for (size_t i = 0; i + 4 <= ws.n; i += 4) words += memcmp(ws.p + i, "\xFF\xFF\xFF\xFF", 4) != 0;
+    fprintf(stderr, "records %zu of %zu\n", words / 130, ws.n / 520);
   }
   return 0;
 }
