@@ -233,7 +233,7 @@ __device__ __forceinline__ SeqSpan seq_span(const PageAttn& a, int s) {   // not
   const int q0 = a.q_start[s], q1 = a.q_start[s + 1], kv = a.kv_len[s];
   SeqSpan r;
   r.q0 = max(q0, 0);
-  r.nq = min(q1, a.n_tokens) - r.q0;
+  r.nq = min(max(q1, 0), a.n_tokens) - r.q0;   // (both at least 0: below 2^31 apart)
   r.kv = (int)min((long long)max(kv, 0), (long long)a.width << a.geom.shift);
   return r;
 }

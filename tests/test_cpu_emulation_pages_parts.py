@@ -75,3 +75,26 @@ def test_parts_are_joined(runs, name):
     for k in kernels:
         assert any(x.startswith(k) for x in ran), (k, ran)
     assert int(re.search(r"^records (\d+) of", r.stderr, re.M).group(1)) == records, r.stderr[-500:]
+
+
+LEAST, MOST = -2 ** 31, 2 ** 31 - 1
+STARTS = [   # q_start of sequences that a case has, where it does not ascend: rows that nobody has are left alone, and nothing outside the arrays is read
+    ([(40, 800)], 200, [200, LEAST], "none"),                            # a difference that leaves 32 bits
+    ([(40, 800)], 200, [MOST, LEAST], "none"),
+    ([(40, 800)], 200, [300, 299], "none"),
+    ([(40, 90), (1, 800)], 150, [190, LEAST, LEAST], "none"),
+    ([(40, 90), (1, 40)], 150, [LEAST, MOST, 0], "any"),                 # the first has all rows
+    ([(1 + 33 * (i == 5), 40) for i in range(66)], 150, [LEAST if i % 2 else 150 + i for i in range(67)], "any"),
+]
+
+
+@pytest.mark.parametrize("i", range(len(STARTS)))
+def test_starts_that_do_not_ascend(i, emulator, tmp_path):
+    seqs, pad, starts, rows = STARTS[i]
+    c = Case("starts", F16, 8, 64, 16, 1, 1, seqs, pad=pad)
+    s = make_inputs(c, str(tmp_path))
+    torch.tensor(starts, dtype=torch.int32).numpy().tofile(str(tmp_path / "q_start.bin"))
+    r = subprocess.run([emulator, str(tmp_path)], capture_output=True, text=True, timeout=900, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"))
+    assert r.returncode == 0 and "Sanitizer" not in r.stderr and "runtime error" not in r.stderr, r.stderr[-4000:]
+    got = torch.from_numpy(np.fromfile(str(tmp_path / "out.bin"), np.uint8)).view(F16).view(s["out"].shape)
+    assert rows == "any" or bool((got == 77.0).all())
