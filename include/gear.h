@@ -315,7 +315,7 @@ int gear_page_attn_bytes(const gear_page_config* cfg, int32_t H_q, const gear_pa
  *     out = softmax(scale * q K^T) V  over the values the pages' rows stand for;
  * query head j reads KV head j / (H_q / H_kv).  Any mix of single tokens, a few rows and whole chunks.  A row that
  * sees nothing is 0.  Scores, softmax statistics and sums are held in fp32; the weights are rounded to the
- * cache's type for the product with V.  A Value that is not finite makes NaN of rows of its sequence that are masked from it, too
+ * cache's type for the product with V (fp16: by half a step of 2^-10 of each down to 2^-21 of a row's greatest, by 2^-32 of that below).  A Value that is not finite makes NaN of rows of its sequence that are masked from it, too
  * (their weight for it is 0); what lies in slots past kv_len does not matter.
  * q, out    : rows [n_tokens][H_q][128] (seq strides not used), dtype of cfg.
  * H_q       : a multiple of H_kv.

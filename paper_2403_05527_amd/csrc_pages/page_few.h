@@ -157,7 +157,7 @@ __device__ __forceinline__ void few_columns(const PageAttn& a, int bid, unsigned
   const int all_see = row_sees(a, sp, 0);   // every column sees the keys before this one
 
   floatx4 o[NC][8];
-  float m[NC], l[NC];
+  float m[NC], l[NC];   // (m: weights_base)
 #pragma unroll
   for (int n = 0; n < NC; ++n) {
     m[n] = -INFINITY;
@@ -226,7 +226,7 @@ __device__ __forceinline__ void few_columns(const PageAttn& a, int bid, unsigned
         for (int i = 0; i < 4; ++i) {
           top = fmaxf(top, score[n][b][i]);
         }
-      top = col_max<true>(top) * a.scale_log2;
+      top = weights_base<BF>(col_max<true>(top) * a.scale_log2, F16_WEIGHT_LOG2);
       if (__ballot(top > m[n]) != 0ull) {
         const float now = fmaxf(m[n], top), by = now == -INFINITY ? 1.0f : GEAR_EXP2(m[n] - now);
         m[n] = now;
@@ -243,7 +243,7 @@ __device__ __forceinline__ void few_columns(const PageAttn& a, int bid, unsigned
           p[4 * b + i] = GEAR_EXP2(__builtin_fmaf(score[n][b][i], a.scale_log2, -from));
           l[n] += p[4 * b + i];
         }
-      // rounded to the type for the product (2^-11 or 2^-8 of each weight, as the outputs are); the sum keeps them in fp32
+      // rounded to the type for the product (F16_WEIGHT_LOG2); the sum keeps them in fp32
       pw[n] = make_uint4(pack2<BF>(p[0], p[1]), pack2<BF>(p[2], p[3]), pack2<BF>(p[4], p[5]), pack2<BF>(p[6], p[7]));
     }
 #pragma unroll

@@ -11,8 +11,8 @@
 // Two tiles: the next one's rows are requested once this one's scores are under way (copied straight into LDS at 16 bits; the
 // compiler lets no LDS read pass a copy that is on its way, so a request at the top of the step would be waited for at once).
 //
-// The maximum that the weights are taken from is raised only when a score exceeds it by more than 8 (in powers of two): weights are
-// then at most 256, exact enough in either type, and the 64 accumulators are rarely rescaled.
+// The maximum that the weights are taken from is raised only when a score exceeds it by more than 8 (in powers of two), so that the 64 accumulators
+// are rarely rescaled; it lies 7 (fp16) or 0 below the score that raised it, so that no weight is above 2^15 or 2^8.
 //
 // A wave that has products to issue goes before one that is in its exponentials (of the two on a SIMD): a prompt of 8192 tokens, 64 heads over 8,
 // 547 -> 534 us; chunks of 512 behind 4096, 32 heads, 187 -> 176 us.  Not beside blocks of few columns, whose loads then go out late (33 sequences of
@@ -268,8 +268,7 @@ __device__ __forceinline__ void many_columns(const PageAttn& a, int bid, unsigne
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[b][i]);
-      top = col_max<false>(top);
-      top *= a.scale_log2;
+      top = weights_base<BF>(col_max<false>(top) * a.scale_log2, F16_WEIGHT_LOG2 - MANY_SLACK);
       if (__ballot(top > m + MANY_SLACK) != 0ull) {   // (from -inf on: any score)
         const float now = fmaxf(m, top), by = now == -INFINITY ? 1.0f : GEAR_EXP2(m - now);
         m = now;
@@ -288,7 +287,7 @@ __device__ __forceinline__ void many_columns(const PageAttn& a, int bid, unsigne
           p[i] = GEAR_EXP2(__builtin_fmaf(sc[u >> 1][8 * (u & 1) + i], a.scale_log2, -from));
           l += p[i];
         }
-        // rounded to the type for the product (2^-11 or 2^-8 of each weight, as the outputs are); the sum keeps them in fp32
+        // rounded to the type for the product (F16_WEIGHT_LOG2); the sum keeps them in fp32
         pw[u] = make_uint4(pack2<BF>(p[0], p[1]), pack2<BF>(p[2], p[3]), pack2<BF>(p[4], p[5]), pack2<BF>(p[6], p[7]));
       }
       if (ALONE) GEAR_WAVE_PRIO(1);

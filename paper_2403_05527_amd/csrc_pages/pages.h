@@ -201,7 +201,7 @@ struct PageAttn {
   const int32_t* table;
   RowView q, out;
   float* rec_o;      // [record rows][n_split][128] partial sums
-  float2* rec_ml;    // [record rows][n_split] (maximum, sum of weights), in units of log2
+  float2* rec_ml;    // [record rows][n_split] (what the weights' exponents are taken from, sum of weights), in units of log2
   float scale_log2;  // |scale| * log2(e), above 0: scores are compared before they are scaled, and -inf times it is -inf
   uint32_t flip;     // 0x80008000 where the scale is negative: the queries change sign instead
   int32_t width;     // entries of a sequence's row of the table
@@ -213,6 +213,10 @@ struct PageAttn {
   int32_t tiles;     // column tiles of page_attn_many_kernel, at most
 };
 constexpr int KEY_STEP = 32, MANY_COLS = 128, MANY_KEYS = 64;
+// The weights' rounding to the type for the product with V: half a step, 2^-11 (fp16) or 2^-8 (bf16) of each, as the outputs'.  fp16 numbers below 2^-14 have
+// fewer bits, and below 2^-25 none: the weights are held times 2^15 for the greatest that there can be, so that a long tail of small ones counts in the product with V
+// as it counts in their sum (held up to 1, 131072 weights of 2^-26 beside one of 1 were 2^-9 of the sum and nothing of the product).
+constexpr float F16_WEIGHT_LOG2 = 15.0f;
 constexpr int FEW_PART = 256, MANY_PART = 128;   // tokens of a part, at least (of few columns: one step of a block's waves)
 
 // The key axis of `keys` tokens in at most n_split equal parts of about `least` tokens and more, multiples of `unit`: tokens of a part, and how many
@@ -269,6 +273,12 @@ __device__ __forceinline__ int page_of(PageRow& r, int key) {
   return __builtin_amdgcn_readlane(r.held, i - r.base);
 }
 __device__ __forceinline__ uint4 signed_query(const uint4& q, uint32_t flip) { return make_uint4(q.x ^ flip, q.y ^ flip, q.z ^ flip, q.w ^ flip); }
+// What the exponents of a column's weights are taken from, whose greatest score is `top` (times log2(e)): `below` less than it in fp16.  Not from 2^23 on, where the
+// base is a whole number and the greatest weight off by as many powers of two as it is rounded by: half a step is 1 from 2^24 on, and fp16 ends at 2^16.
+template <bool BF>
+__device__ __forceinline__ float weights_base(float top, float below) {
+  return !BF && fabsf(top) < 0x1p23f ? top - below : top;
+}
 // Greatest value / sum over the lanes of a column, l % 16 (Q16) or l % 32.
 template <bool Q16>
 __device__ __forceinline__ float col_max(float v) {

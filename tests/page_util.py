@@ -117,3 +117,29 @@ def attend(q, K, V, q_start, kv_len, table, scale, causal):
             b = A * rel + tiny
             out[q0:q1, j], bound[q0:q1, j] = o, b + eps * (o.abs() + b) + (2.0 ** -25 if dtype == torch.float16 else 0.0)
     return out, bound
+
+
+def sink_and_tail(K, V, q, table, kv, page):
+    """In place: the first 256 of kv tokens hold a Key in every 32nd (one for each wave of a block) whose weight is 2^26 times that of all others, and
+    no Value; the others' Values are about 1.  Returns the scale."""
+    K[:], q[:] = 0.0, 1.0
+    V[:] = 0.5 + V.abs().clamp(max=1.0)
+    for i in range(0, 256, 32):
+        p, r = int(table[i // page]), i % page
+        K[p, :, r], V[p, :, r] = 1.0, 0.0
+    assert kv > 256
+    return 26 * math.log(2.0) / 128
+
+
+def tail_bound(q, K, V, table, kv, q0, q1, scale, page):
+    """(out, bound) of one sequence and head in fp16.  A weight is rounded to fp16, half a step 2^-11 of it or, of a subnormal number, 2^-25; the numbers
+    are weights times a power of two that brings a row's greatest to 2^7 at least, so that is 2^-32 of the greatest: of less than the sum."""
+    at = torch.arange(kv)
+    k, v = (X[torch.tensor(table)[at // page].long(), 0, at % page].double() for X in (K, V))
+    sc = q[q0:q1, 0].double() @ k.t() * scale
+    sc = sc.masked_fill(at[None] >= (kv - (q1 - q0) + 1 + torch.arange(q1 - q0))[:, None], -math.inf)
+    p = torch.softmax(sc, -1)
+    o = p @ v
+    # fp32: a score of at most 18 (its products are exact), the exponent's argument and exp2, sums of kv terms
+    b = o * (2.0 ** -11 + (kv + 64 + 18) * 2.0 ** -23) + kv * 2.0 ** -32 * v.amax()
+    return o, b + (o + b) * 2.0 ** -11 + 2.0 ** -25

@@ -1,5 +1,6 @@
 """The paged cache's attention on the CPU stand-in (tests/simt/) with the plans that it makes for the 256 CUs of the device, so that axes are
 divided and their parts joined: under the address sanitizer, 16-byte stores looked at for their alignment, on buffers of exactly their size, against the definition in 64 bits."""
+import math
 import os
 import re
 import subprocess
@@ -35,7 +36,7 @@ def emulator(tmp_path_factory):
 
 
 def launches(err):
-    """{kernel with its template arguments: blocks}"""
+    """{kernel as the launch names it: blocks}"""
     return {k: int(n) for k, n in re.findall(r"^launch (\w+(?:<[^>]*>)?)\)? grid (\d+)", err, re.M)}
 
 
@@ -98,3 +99,49 @@ def test_starts_that_do_not_ascend(i, emulator, tmp_path):
     assert r.returncode == 0 and "Sanitizer" not in r.stderr and "runtime error" not in r.stderr, r.stderr[-4000:]
     got = torch.from_numpy(np.fromfile(str(tmp_path / "out.bin"), np.uint8)).view(F16).view(s["out"].shape)
     assert rows == "any" or bool((got == 77.0).all())
+
+
+def run_with(emulator, path, c, s, scale):
+    """The case with s's Keys, Values and queries, 16 bits, one head, and this scale: [rows, 128] in 64 bits."""
+    c.scale = scale
+    meta = (path / "meta.txt").read_text().split()
+    meta[7] = repr(scale)
+    (path / "meta.txt").write_text(" ".join(meta) + "\n")
+    blocks = torch.stack([pg.pack(x, 16, 128, c.dtype) for x in (s["K"], s["V"])], 2)
+    for name, t in (("pool.bin", blocks), ("q.bin", s["q"])):
+        t.contiguous().view(torch.uint8).numpy().tofile(str(path / name))
+    r = subprocess.run([emulator, str(path)], capture_output=True, text=True, timeout=900, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"))
+    check(c, str(path), s, r)
+    assert [k.split("<")[0] for k in launches(r.stderr)] == ["page_attn_few_kernel" if len(s["q"]) == 1 else "page_attn_many_kernel"], r.stderr
+    return torch.from_numpy(np.fromfile(str(path / "out.bin"), np.uint8)).view(c.dtype).view(s["out"].shape)[:, 0].double()
+
+
+@pytest.mark.parametrize("n", [1, 36])
+def test_a_flat_tail_counts(n, emulator, tmp_path):
+    """Many weights that are each far below a row's greatest, in the sum of Values as in the sum of weights: one token, and a chunk."""
+    kv, page = 1536, 16
+    c = Case("tail", F16, 16, 128, page, 1, 1, [(n, kv)], max_kv=1)     # (one part)
+    s = make_inputs(c, str(tmp_path))
+    scale = pg.sink_and_tail(s["K"], s["V"], s["q"], s["table"][0], kv, page)
+    got = run_with(emulator, tmp_path, c, s, scale)
+    want, bound = pg.tail_bound(s["q"], s["K"], s["V"], s["table"][0], kv, 0, n, scale, page)
+    assert float(want.min()) > 2.0 ** -20         # 1500 of 2^-26, each with a Value of 1/2 and more, beside 8 of 1
+    assert bool(((got - want).abs() <= bound).all()), float(((got - want).abs() / bound).max())
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("n", [1, 36])
+@pytest.mark.parametrize("log2", [15.3, 22.97, 23.02, 24.3, 25.7, 27.4])
+def test_equal_scores_of_any_size(log2, n, dtype, emulator, tmp_path):
+    """All scores equal, from 2^15 to 2^27 steps of the exponent: the mean of the Values, however the base of the weights is rounded."""
+    kv, page = 70, 16
+    c = Case("equal", dtype, 16, 128, page, 1, 1, [(n, kv)], causal=False)
+    s = make_inputs(c, str(tmp_path))
+    s["K"][:], s["q"][:] = 512.0, 512.0                                 # (sums of products are exact)
+    got = run_with(emulator, tmp_path, c, s, 2.0 ** (log2 - 25) * math.log(2.0))
+    at = torch.arange(kv)
+    v = s["V"][torch.tensor(s["table"][0])[at // page], 0, at % page].double()
+    # one weight for all tokens, but rounded before the product and not before the sum; 70 terms in fp32
+    eps, most = torch.finfo(dtype).eps / 2, v.abs().mean(0)
+    bound = most * (eps + 80 * 2.0 ** -23)
+    assert bool(((got - v.mean(0)).abs() <= bound + (v.mean(0).abs() + bound) * eps + 2.0 ** -25).all())
