@@ -246,9 +246,11 @@ int gear_export_sparse_coo(const gear_cache* cache, int which, int64_t* nnz, voi
  *   8 bits: byte c of the row is channel c's code;
  *   4 bits: channel 8 w + e is word w's bits 4 (e / 2) + 16 (e % 2) and the three above;
  * and behind the code rows (scale, zero) words u32 [128 / group][page_size], scale in the low half, both
- * of the cache's type.  A code stands for the value  scale * code + zero  rounded to the cache's type, with
+ * of the cache's type.  A code stands for the value  scale * code + zero,  rounded to fp16 once, or to fp32 and then to bf16, with
  *   zero = min x,  scale = (max x - min x) / (2^b - 1) rounded to the cache's type (the quotient in fp32),
- *   code = the integer nearest to (x - zero) / scale, halves to even, at most 2^b - 1; 0 where scale is 0
+ *   code = the integer nearest to (x - zero) / scale, halves to even, at most 2^b - 1; 0 where scale is 0.  The difference x - zero is
+ *   rounded to fp32 first: where one of the two is so small beside the other (below 2^-12 of it in fp16, 2^-15 in bf16) that fp32 does
+ *   not hold it, and what it is rounded to is an odd half of the scale, the code is the even one of two that are all but equally near,
  * over the group's entries x (Eq. 2).  Slot i is row i % page_size of page i / page_size.
  */
 typedef enum gear_dtype { GEAR_F16 = 0, GEAR_BF16 = 1 } gear_dtype;

@@ -64,10 +64,10 @@ __device__ __forceinline__ void store_piece(const PageGeom& g, unsigned char* bl
     const uint32_t sz = (pack2<BF>(s32, 0.0f) & 0xFFFFu) | zero << 16;
     const float scale = to_f32<BF>(sz & 0xFFFFu);
     uint32_t code[8];
-    // (x - zero) / scale as IEEE division gives it, in a product and two fused steps: with a correctly rounded reciprocal the last one rounds
-    // the exact quotient.  The difference is exact unless the exponents lie more than 13 (bf16: 16) apart, and such a quotient is rounded
-    // across a half only where it lies within 2^-17 of one.  Then the nearest integer is the sum with 1.5 * 2^23, whose last bits
-    // are the code.  (Dividing: 8 x 4096 tokens of 8 heads to 4 bits 58 us.)
+    // (x - zero) / scale as IEEE division in fp32 gives it, in a product and two fused steps: with a correctly rounded reciprocal the last one rounds
+    // the exact quotient, which by a scale of 11 bits or 8 is never rounded to a half that it is not.  The difference is exact unless the exponents lie more than
+    // 12 (bf16: 15) apart; one that is not, and is rounded to a half of the scale, gets the even code (include/gear.h).  Then the nearest integer is the sum with
+    // 1.5 * 2^23, whose last bits are the code.  (Dividing: 8 x 4096 tokens of 8 heads to 4 bits 58 us.)
     // A scale is off by 2^-11 (fp16) or 2^-8 (bf16) of it, more where it is denormal: only of these and of 8-bit codes in bf16 may a quotient come to more than half
     // a step past the last code.
     const float inv = scale > 0.0f ? recip_of_half(scale) : 0.0f;

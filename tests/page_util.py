@@ -143,3 +143,54 @@ def tail_bound(q, K, V, table, kv, q0, q1, scale, page):
     # fp32: a score of at most 18 (its products are exact), the exponent's argument and exp2, sums of kv terms
     b = o * (2.0 ** -11 + (kv + 64 + 18) * 2.0 ** -23) + kv * 2.0 ** -32 * v.amax()
     return o, b + (o + b) * 2.0 ** -11 + 2.0 ** -25
+
+
+def quantise_fp32(x, bits, group, dtype):
+    """(codes, scale, zero) as include/gear.h states them, in its own arithmetic: the difference and the quotient in fp32.  (Against quantise above: where the
+    difference is not exact in fp32 and rounds to a half of the scale.)"""
+    x = x.float().unflatten(-1, (D // group, group))
+    zero, top = x.amin(-1), x.amax(-1)
+    scale = ((top - zero) / torch.tensor(float(2 ** bits - 1))).to(dtype).float()
+    code = torch.where(scale[..., None] > 0, (x - zero[..., None]) / torch.where(scale > 0, scale, 1.0)[..., None], 0.0).round().clamp(0, 2 ** bits - 1)
+    return code.flatten(-2).long(), scale.to(dtype), zero.to(dtype)
+
+
+def values_fp32(code, scale, zero, group, dtype):
+    """What codes stand for as include/gear.h states it: rounded once in fp16, to fp32 first in bf16."""
+    if dtype == torch.float16:
+        return stored_values(code, scale, zero, group, dtype)
+    s, z = (t.float().repeat_interleave(group, -1) for t in (scale, zero))
+    return (code.float() * s + z).to(dtype)                  # (the product is exact)
+
+
+def block_of_codes(code, scale, zero, bits):
+    """Block bytes [..., bytes] of codes [..., page, 128] and their words."""
+    if bits == 8:
+        rows = code.to(torch.uint8)
+    else:
+        word = sum(code[..., e::8] << (4 * (e // 2) + 16 * (e % 2)) for e in range(8))
+        rows = torch.stack([(word >> (8 * k)) & 255 for k in range(4)], -1).to(torch.uint8)
+    words = torch.stack((scale, zero), -1).transpose(-3, -2).contiguous().view(torch.uint8)
+    lead = code.shape[:-2]
+    return torch.cat((rows.reshape(*lead, -1), words.reshape(*lead, -1)), -1)
+
+
+def rows_at_ties(bits, dtype):
+    """Rows [n, 128] (every group of 32 alike) whose differences from their least value are halves of the scale but for less than fp32 holds, and the codes that the
+    difference rounded to fp32 gives them; the exact ones differ."""
+    levels, tiny = 2 ** bits - 1, 2.0 ** -24 if dtype == torch.float16 else 2.0 ** -40
+    rows, codes = [], []
+    for s in (1.0, 0.5, 2.0):
+        # the least value next to nothing: (k + 1/2) s above or below a half, which go to the even side alike
+        for sign in (-1, 1):
+            for k in range(2, 12):
+                if (k % 2 == 0) == (sign < 0):               # rounded to even is the other side
+                    rows.append([sign * tiny, levels * s, (k + 0.5) * s] + [s] * 29)
+                    codes.append((k if k % 2 == 0 else k + 1, k + 1 if k % 2 == 0 else k))
+        # a value next to nothing, the least one halves of the scale
+        if bits == 4 or dtype == torch.float16:              # (a bf16 number has eight bits: levels - k - 1/2 needs nine)
+            for k in (2, 4):
+                rows.append([-(k + 0.5) * s, (levels - k - 0.5) * s, tiny] + [s * 0.5] * 29)
+                codes.append((k, k + 1))
+    x = torch.tensor(rows, dtype=torch.float64).repeat(1, 4).to(dtype)
+    return x, codes

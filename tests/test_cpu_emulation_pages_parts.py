@@ -145,3 +145,41 @@ def test_equal_scores_of_any_size(log2, n, dtype, emulator, tmp_path):
     eps, most = torch.finfo(dtype).eps / 2, v.abs().mean(0)
     bound = most * (eps + 80 * 2.0 ** -23)
     assert bool(((got - v.mean(0)).abs() <= bound + (v.mean(0).abs() + bound) * eps + 2.0 ** -25).all())
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("bits", [8, 4])
+def test_codes_and_values_at_ties(bits, dtype, emulator, tmp_path):
+    """The codes of a difference that fp32 does not hold, and the values of a sum that it does not hold: as stated.  And the pool's bytes, of slots that were
+    named and of such that were not."""
+    x, codes = pg.rows_at_ties(bits, dtype)
+    if bits == 4 and dtype == BF16:
+        x = torch.cat((torch.tensor([-2.0 ** -30, 15.125, 3.015625] + [0.5] * 29, dtype=torch.float64).repeat(1, 4).to(dtype), x))
+    n, page = len(x), 16
+    c = Case("ties", dtype, bits, 32, page, 1, 1, [(0, n)], write=True)
+    s = make_inputs(c, str(tmp_path))
+    new = torch.stack((x, -x.flip(0)))                                   # Keys; Values
+    for name, t in zip(("K.bin", "V.bin"), new):
+        t.contiguous().view(torch.uint8).numpy().tofile(str(tmp_path / name))
+    r = subprocess.run([emulator, str(tmp_path)], capture_output=True, text=True, timeout=900, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"))
+    assert r.returncode == 0 and "Sanitizer" not in r.stderr, r.stderr[-4000:]
+    code, scale, zero = pg.quantise_fp32(new, bits, 32, dtype)
+    assert [(int(code[0, i, 2]), int(pg.quantise(x, bits, 32, dtype)[0][i, 2])) for i in range(n - len(codes), n)] == codes
+    values = pg.values_fp32(code, scale, zero, 32, dtype)
+    if bits == 4 and dtype == BF16:
+        assert values[0, 0, 2] == 3.03125 and pg.stored_values(code, scale, zero, 32, dtype)[0, 0, 2] == 3.015625
+    slots = s["slots"][0]
+    live = (slots >= 0) & (slots < s["pool"].shape[0] * page)
+    assert int(live.sum()) == n - 2
+    for name, v in zip(("K_back.bin", "V_back.bin"), values):
+        got = torch.from_numpy(np.fromfile(str(tmp_path / name), np.uint8)).view(dtype).view(n, 128)
+        assert torch.equal(got[live].view(torch.int16), v[live].contiguous().view(torch.int16))
+    rb, want = 128 * bits // 8, s["pool"].clone()                        # [pages, 1, 2, bytes]
+    block = pg.block_of_codes(code[:, :, None], scale[:, :, None], zero[:, :, None], bits)      # a block of one row each
+    for i, slot in enumerate(slots.tolist()):
+        if live[i]:
+            p, row = slot // page, slot % page
+            want[p, 0, :, row * rb:(row + 1) * rb] = block[:, i, :rb]
+            want[p, 0, :, page * rb:].view(2, 4, page, 4)[:, :, row] = block[:, i, rb:].view(2, 4, 4)
+    after = torch.from_numpy(np.fromfile(str(tmp_path / "pool_after.bin"), np.uint8)).view(want.shape)
+    assert torch.equal(after, want)

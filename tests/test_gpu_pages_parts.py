@@ -44,3 +44,41 @@ def test_equal_scores_of_any_size(log2, n, dtype):
     for max_kv in (1, 100000):
         got = attn(c, scale=2.0 ** (log2 - 25) * math.log(2.0), causal=False, max_kv=max_kv)[:, 0].cpu().double()
         assert bool(((got - v.mean(0)).abs() <= bound + (v.mean(0).abs() + bound) * eps + 2.0 ** -25).all())
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("bits", [8, 4])
+def test_codes_and_values_at_ties(bits, dtype):
+    """The codes of a difference that fp32 does not hold, and the values of a sum that it does not hold: as stated."""
+    x, _ = pg.rows_at_ties(bits, dtype)
+    if bits == 4 and dtype == BF16:
+        x = torch.cat((torch.tensor([-2.0 ** -30, 15.125, 3.015625] + [0.5] * 29, dtype=torch.float64).repeat(1, 4).to(dtype), x))
+    n, page = len(x), 64
+    new = torch.stack((x, -x.flip(0)))                                   # Keys; Values
+    pool = gb.PagePool(gb.make_page_config(1, page, 1, bits, 32, dtype), DEV)
+    slots = torch.arange(n, device=DEV)
+    pool.write(new[0][:, None].to(DEV), new[1][:, None].to(DEV), slots)
+    code, scale, zero = pg.quantise_fp32(torch.cat((new, torch.zeros(2, page - n, 128, dtype=dtype)), 1), bits, 32, dtype)
+    assert torch.equal(pool.pool.cpu(), pg.block_of_codes(code, scale, zero, bits).reshape(-1))
+    values = pg.values_fp32(code, scale, zero, 32, dtype)[:, :n]
+    for got, v in zip(pool.read(slots[None]), values):
+        assert torch.equal(got[0, :, 0].cpu().view(torch.int16), v.contiguous().view(torch.int16))
+    # a token that sees one key alone gets its Value (a score of 0: its weight is a power of two)
+    b = gb.make_page_batch(*(torch.tensor(t, dtype=torch.int32, device=DEV) for t in ((0, 1), (1,), ((0,),))), 1, 1, page)
+    for i in range(0, n, 5):
+        one = gb.PagePool(pool.cfg, DEV)
+        one.write(new[0][i:i + 1, None].to(DEV), new[1][i:i + 1, None].to(DEV), slots[:1])
+        out = one.attn(torch.zeros(1, 1, 128, dtype=dtype, device=DEV), b)
+        assert torch.equal(out.cpu().view(torch.int16).view(-1), values[1, i].contiguous().view(torch.int16))
+
+
+def test_a_bf16_sum_goes_through_fp32():
+    """8-bit codes whose value is half a bf16 step but for what fp32 does not hold."""
+    page = 16
+    code = torch.full((2, page, 128), 3)
+    scale = torch.full((2, page, 4), 1.0078125).to(BF16)
+    zero = torch.full((2, page, 4), -2.0 ** -30).to(BF16)
+    pool = gb.PagePool(gb.make_page_config(1, page, 1, 8, 32, BF16), DEV)
+    pool.pool.copy_(pg.block_of_codes(code, scale, zero, 8).reshape(-1))
+    K, V = pool.read(torch.arange(page, device=DEV)[None])
+    assert bool((K == 3.03125).all()) and bool((V == 3.03125).all())     # (once: 3.015625)
