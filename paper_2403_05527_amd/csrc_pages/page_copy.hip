@@ -119,10 +119,16 @@ constexpr int COPY_THREADS = 256, COPY_ROWS = COPY_THREADS / 16;
 #ifndef GEAR_PAGE_PAST_CACHES   // (the CPU stand-in lowers it)
 #define GEAR_PAGE_PAST_CACHES (64ll << 20)
 #endif
-constexpr int64_t PAST_CACHES = GEAR_PAGE_PAST_CACHES;   // bytes of both tensors
+constexpr int64_t PAST_CACHES = GEAR_PAGE_PAST_CACHES;   // bytes that are brought back
 
-// What is brought back once and is larger than the caches is stored past them (7 x 1777 tokens of 40 heads, 255 MB: 79 -> 47 us;
-// 16 x 4096 of 32, 1.07 GB: 314 -> 289).
+// What is brought back and is large is stored past the caches, which keep what they held: behind the write of the same rows (8 x 4096 tokens of 8 heads, 128 MiB, 4
+// bits) both take 60 us, and 69 into the caches; 7 x 1777 tokens of 40 heads, 255 MB, 79 -> 47; 16 x 4096 of 32, 1.07 GB, 314 -> 289.  A kernel that reads the rows at once
+// would find part of less than 256 MB there, and pays for it.  In us, 8 KV heads, groups of 64, into the caches and past them: the read by itself, and with a maximum
+// over each tensor behind it:
+//   MiB               64                 128                192                256                512
+//   fp16 at 8 bits    15 14, 57 66       26 25, 89 108      60 37, 142 155     82 49, 220 223     160 148, 437 421
+//   bf16 at 4 bits    14 13, 57 67       24 22, 89 108      40 32, 136 151     87 46, 217 228     164 79, 453 432
+//   fp16 at 16 bits   18 18, 60 69       35 34, 98 117      77 49, 168 173     103 64, 240 243    199 196, 471 471
 template <bool PAST>
 __device__ __forceinline__ void store16(unsigned char* p, const uint4& v) {
 #ifdef GEAR_NO_NONTEMPORAL
@@ -172,7 +178,7 @@ __global__ __launch_bounds__(COPY_THREADS) void page_copy_kernel(PageCopy a) {
 template <int BITS, bool BF, bool WRITE>
 static hipError_t launch_copy(const PageCopy& a, int n_seqs, hipStream_t st) {
   const int64_t blocks = (int64_t)n_seqs * a.chunks * a.geom.H;
-  if (!WRITE && (int64_t)n_seqs * a.n_rows * a.geom.H * (4 * D) >= PAST_CACHES)
+  if (!WRITE && (int64_t)n_seqs * a.n_rows * a.geom.H * ((a.k.data ? 2 * D : 0) + (a.v.data ? 2 * D : 0)) >= PAST_CACHES)
     hipLaunchKernelGGL((page_copy_kernel<BITS, BF, WRITE, !WRITE>), dim3((unsigned)blocks), dim3(COPY_THREADS), 0, st, a);
   else
     hipLaunchKernelGGL((page_copy_kernel<BITS, BF, WRITE, false>), dim3((unsigned)blocks), dim3(COPY_THREADS), 0, st, a);

@@ -183,3 +183,16 @@ def test_codes_and_values_at_ties(bits, dtype, emulator, tmp_path):
             want[p, 0, :, page * rb:].view(2, 4, page, 4)[:, :, row] = block[:, i, rb:].view(2, 4, 4)
     after = torch.from_numpy(np.fromfile(str(tmp_path / "pool_after.bin"), np.uint8)).view(want.shape)
     assert torch.equal(after, want)
+
+
+def test_bytes_of_the_tensors_that_are_read(emulator, tmp_path):
+    """Rows are stored past the caches from a number of bytes on (32 KB in the stand-in), of Keys and Values together where both are brought back: each of
+    the two reads here brings back one, of 79 rows and 20 KB, or of 128 and 32."""
+    for rows, past in ((79, False), (128, True)):
+        d = tmp_path / str(rows)
+        d.mkdir()
+        make_inputs(Case("past", F16, 8, 64, 16, 1, 1, [(0, rows)], write=True), str(d))
+        r = subprocess.run([emulator, str(d)], capture_output=True, text=True, timeout=900, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"))
+        assert r.returncode == 0, r.stderr[-2000:]
+        reads = re.findall(r"^launch page_copy_kernel<BITS, BF, WRITE, (\S+)>", r.stderr, re.M)
+        assert reads == ["false"] + ["!WRITE" if past else "false"] * 2, r.stderr[-2000:]
