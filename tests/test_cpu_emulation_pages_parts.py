@@ -44,6 +44,16 @@ def launches(err):
 PARTS = {c.name: (c, kernels, records) for c, kernels, records in [
     # 34 columns in 5 parts, 175 records in the workspace, and one in 3: an odd number of records lies before those of the few columns
     (Case("both_odd", F16, 16, 128, 16, 1, 1, [(34, 800), (1, 790)]), ["page_attn_mixed_kernel", "page_merge_many_kernel<1>", "page_merge_few_kernel"], 34 * 5 + 3),
+    # 9 parts, and 5
+    (Case("both_four_waves", BF16, 8, 64, 16, 1, 1, [(34, 1700), (1, 1690)]), ["page_attn_mixed_kernel", "page_merge_many_kernel<4>", "page_merge_few_kernel"], 34 * 9 + 5),
+    (Case("few", F16, 8, 128, 16, 1, 2, [(1, 1100), (1, 30)], bad=True), ["page_attn_few_kernel", "page_merge_few_kernel"], 2 * 3),
+    (Case("few_two_tiles", F16, 4, 32, 16, 1, 10, [(2, 1100), (1, 600)]), ["page_attn_few_kernel", "page_merge_few_kernel"], 20 * 3 + 10 * 2),
+    # more records than the four waves of a merge ask for at a time (32), and than a wave's lanes look at (64)
+    (Case("few_34_parts", F16, 4, 128, 256, 1, 1, [(1, 17000)]), ["page_attn_few_kernel", "page_merge_few_kernel"], 34),
+    (Case("few_65_parts", F16, 4, 128, 256, 1, 1, [(1, 33000)]), ["page_attn_few_kernel", "page_merge_few_kernel"], 65),
+    (Case("many_68_parts", F16, 16, 128, 256, 1, 1, [(33, 13000)]), ["page_attn_many_kernel", "page_merge_many_kernel<4>"], 33 * 68),
+    # the joining looks for a row's sequence among more than a wave has lanes
+    (Case("many_of_66", F16, 8, 128, 16, 1, 1, [(34, 1500) if i == 64 else (1, 17 + i % 3) for i in range(66)]), ["page_attn_mixed_kernel", "page_merge_many_kernel<1>"], 34 * 8),
 ]}
 
 
@@ -65,6 +75,23 @@ def check(c, d, s, r):
     dead = torch.isnan(want)
     assert bool((got[dead] == 77.0).all())
     assert bool(((got - want).abs() <= bound)[~dead].all()), float(((got - want).abs() / bound)[~dead].max())
+
+
+# a part's pages are more than a wave's lanes hold at a time (64): tables of 94 entries, some of no page, one part
+ENTRIES = [(n, form) for n in (1, 40) for form in ((F16, 16, 128), (F16, 4, 32), (BF16, 8, 64))]
+
+
+@pytest.mark.parametrize("n,form", ENTRIES)
+def test_pages_past_the_first_look(n, form, emulator, tmp_path):
+    dtype, bits, group = form
+    c = Case("entries", dtype, bits, group, 16, 1, 1, [(n, 1500), (n, 1040)], max_kv=1)
+    s = make_inputs(c, str(tmp_path))
+    for i, page in ((3, -1), (64, -7), (70, 10 ** 6), (71, s["pool"].shape[0]), (93, -1)):
+        s["table"][0][i] = page
+    torch.tensor(s["table"], dtype=torch.int32).numpy().tofile(str(tmp_path / "table.bin"))
+    r = subprocess.run([emulator, str(tmp_path)], capture_output=True, text=True, timeout=900, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"))
+    check(c, str(tmp_path), s, r)
+    assert len(launches(r.stderr)) == 1, r.stderr
 
 
 @pytest.mark.parametrize("name", list(PARTS))

@@ -82,3 +82,47 @@ def test_a_bf16_sum_goes_through_fp32():
     pool.pool.copy_(pg.block_of_codes(code, scale, zero, 8).reshape(-1))
     K, V = pool.read(torch.arange(page, device=DEV)[None])
     assert bool((K == 3.03125).all()) and bool((V == 3.03125).all())     # (once: 3.015625)
+
+
+LONG = [   # page, H, gq, sequences (new tokens, tokens), padding rows
+    (16, 1, 1, [(34, 800), (1, 790)], 0),                                 # an odd number of records before those of the few columns
+    (16, 1, 1, [(301, 9000), (2, 8999)], 1),
+    (16, 1, 1, [(1, 9000)], 0),                                           # more parts than a merge's waves ask for at a time (32) ...
+    (32, 1, 3, [(1, 40000)], 0),                                          # ... than a wave's lanes look at (64)
+    (64, 1, 2, [(20, 14000)], 0),                                         # the same of many columns
+    (16, 1, 1, [(34, 1500) if i == 64 else (1, 17 + i % 3) for i in range(66)], 0),   # the joining looks for a row among more than 64 sequences
+    (16, 2, 2, [(1 + (i % 30 == 7) * 50, 40 + 7 * i) for i in range(130)], 2),
+]
+
+
+@pytest.mark.parametrize("dtype,bits,group", [(F16, 16, 128), (BF16, 8, 64), (F16, 4, 32)])
+@pytest.mark.parametrize("i", range(len(LONG)))
+def test_many_parts(i, dtype, bits, group):
+    page, H, gq, seqs, pad = LONG[i]
+    c = Cache(dtype, bits, group, page, H, gq, seqs, seed=30 + i, pad=pad)
+    c.check(attn(c), before=77.0)
+
+
+@pytest.mark.parametrize("dtype,bits,group", [(F16, 16, 128), (BF16, 8, 64), (F16, 4, 32)])
+@pytest.mark.parametrize("n", [1, 40])
+def test_pages_past_the_first_look(n, dtype, bits, group):
+    """A part's pages are more than a wave's lanes hold at a time (64): tables of 313 entries, some of no page, in one part and as the call divides them."""
+    c = Cache(dtype, bits, group, 16, 2, 1, [(n, 5000), (n, 1040)], seed=40)
+    table = c.table.clone()
+    for e, page in ((3, -1), (64, -7), (70, 10 ** 6), (71, c.cfg.n_pages), (200, -1), (312, -1)):
+        table[0, e] = page
+    for max_kv in (1, None):
+        c.check(attn(c, table=table, max_kv=max_kv), table=table)
+
+
+STARTS = [(200, -2 ** 31), (2 ** 31 - 1, -2 ** 31), (300, 299)]
+
+
+@pytest.mark.parametrize("starts", STARTS)
+def test_starts_that_do_not_ascend(starts):
+    """Rows that nobody has are left alone, and nothing outside the arrays is read."""
+    for seqs in ([(40, 800)], [(40, 800)] * 70):
+        c = Cache(F16, 8, 64, 16, 1, 1, seqs, seed=50, pad=200)
+        b = c.batch()
+        b.tensors[0].copy_(torch.tensor([starts[k % 2] for k in range(len(seqs) + 1)] if len(seqs) == 1 else [starts[0]] + [starts[1]] * len(seqs), dtype=torch.int32))
+        assert bool((attn(c, batch=b) == 77.0).all())
