@@ -11,7 +11,7 @@
 // Bound by the pages' bytes at 16 and 8 bits, by the conversions beside them at 4: one token each of 16 sequences of 4096, 32 heads, groups of 64, fp16 181, 101 and
 // 63 us at 16, 8 and 4 bits (5.9, 5.7 and 4.8 TB/s), bf16, whose values are rounded in fp32, 187, 106 and 69.
 // The keys are divided among the waves of a block and, where the sequences and heads are few, among blocks, whose records
-// page_merge_kernel joins.
+// page_merge_few_kernel joins.
 #pragma once
 #include "pages.h"
 

@@ -5,7 +5,8 @@
 
 namespace gear {
 
-// Eight waves: with four, and twice the blocks, one token behind 32768 took 21 us instead of 18, two tiles of columns 196 instead of 173 in a mixed batch.
+// Eight waves: with four, and twice the blocks, one token behind 32768 took 21 us instead of 18.  (Blocks that share a launch with those of many columns have four:
+// page_mixed.hip.)
 constexpr int FEW_WAVES = 8;
 
 template <int BITS, bool BF, int NC>
