@@ -265,7 +265,8 @@ typedef struct gear_page_config {
   int32_t dtype;      /* gear_dtype of rows, queries and outputs                            */
 } gear_page_config;
 
-/* 16-bit values [n_seqs][tokens][heads][128], the 128 contiguous; strides in elements. */
+/* 16-bit values [n_seqs][tokens][heads][128], the 128 contiguous; strides in elements.  Rows that a call writes must not overlap
+ * (GEAR_EINVAL where two sequences, tokens or heads in a row do, or two strides are the same); rows that it reads may. */
 typedef struct gear_page_rows {
   void*   data;       /* device, 16-byte aligned; strides multiples of 8 */
   int64_t seq;

@@ -139,11 +139,22 @@ int check_pool(const gear_page_config* cfg, const void* pool, size_t pool_bytes,
   return GEAR_OK;
 }
 
-// written: two rows must not share their place (where there are two)
+// Whether rows of these strides lie over one another: within one direction, or one step of two directions in the same place.  (Whatever is laid out one direction
+// after the other does not; strides that overlap in other ways are the caller's.)
+bool rows_overlap(int64_t n_seqs, int64_t seq, int64_t n_rows, int64_t token, int64_t heads, int64_t head) {
+  const int64_t count[3] = {n_seqs, n_rows, heads}, stride[3] = {seq, token, head};
+  for (int i = 0; i < 3; ++i) {
+    if (count[i] <= 1) continue;
+    if (stride[i] < D && stride[i] > -D) return true;
+    for (int j = 0; j < i; ++j)
+      if (count[j] > 1 && (stride[i] == stride[j] || stride[i] == -stride[j])) return true;
+  }
+  return false;
+}
 int check_rows(const gear_page_rows* r, int64_t n_seqs, int64_t n_rows, int64_t heads, bool written) {
   if (!r->data) return GEAR_EINVAL;
   if (misaligned(r->data, 16) || (n_seqs > 1 && r->seq % 8) || (n_rows > 1 && r->token % 8) || (heads > 1 && r->head % 8)) return GEAR_EALIGN;
-  if (written && ((n_seqs > 1 && r->seq == 0) || (n_rows > 1 && r->token == 0) || (heads > 1 && r->head == 0))) return GEAR_EINVAL;
+  if (written && rows_overlap(n_seqs, r->seq, n_rows, r->token, heads, r->head)) return GEAR_EINVAL;
   return GEAR_OK;
 }
 RowView view_of(const gear_page_rows* r) {
