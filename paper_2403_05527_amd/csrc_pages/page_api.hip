@@ -252,6 +252,7 @@ int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_by
   a.q = view_of(q);
   a.out = view_of(out);
   a.scale_log2 = std::fmax(scale_log2, 1e-37f);   // (a scale of 0: every score comes to less than a step of 2^0)
+  a.far = 0x1p23f / a.scale_log2;
   a.flip = scale < 0.0f ? 0x80008000u : 0u;
   a.width = b.table_width;
   a.n_seqs = b.n_seqs;

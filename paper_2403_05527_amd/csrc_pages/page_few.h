@@ -226,7 +226,7 @@ __device__ __forceinline__ void few_columns(const PageAttn& a, int bid, unsigned
         for (int i = 0; i < 4; ++i) {
           top = fmaxf(top, score[n][b][i]);
         }
-      top = weights_base<BF>(col_max<true>(top) * a.scale_log2, F16_WEIGHT_LOG2);
+      top = weights_base<BF>(col_max<true>(top), a.scale_log2, a.far, F16_WEIGHT_LOG2);
       if (__ballot(top > m[n]) != 0ull) {
         const float now = fmaxf(m[n], top), by = now == -INFINITY ? 1.0f : GEAR_EXP2(m[n] - now);
         m[n] = now;

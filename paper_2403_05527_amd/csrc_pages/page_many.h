@@ -269,7 +269,7 @@ __device__ __forceinline__ void many_columns(const PageAttn& a, int bid, unsigne
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[b][i]);
-      top = weights_base<BF>(col_max<false>(top) * a.scale_log2, F16_WEIGHT_LOG2 - MANY_SLACK);
+      top = weights_base<BF>(col_max<false>(top), a.scale_log2, a.far, F16_WEIGHT_LOG2 - MANY_SLACK);
       if (__ballot(top > m + MANY_SLACK) != 0ull) {   // (from -inf on: any score)
         const float now = fmaxf(m, top), by = now == -INFINITY ? 1.0f : GEAR_EXP2(m - now);
         m = now;

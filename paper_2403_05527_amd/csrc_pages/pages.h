@@ -203,6 +203,7 @@ struct PageAttn {
   float* rec_o;      // [record rows][n_split][128] partial sums
   float2* rec_ml;    // [record rows][n_split] (what the weights' exponents are taken from, sum of weights), in units of log2
   float scale_log2;  // |scale| * log2(e), above 0: scores are compared before they are scaled, and -inf times it is -inf
+  float far;         // 2^23 / scale_log2
   uint32_t flip;     // 0x80008000 where the scale is negative: the queries change sign instead
   int32_t width;     // entries of a sequence's row of the table
   int32_t n_seqs, n_tokens, gq, causal;
@@ -273,11 +274,11 @@ __device__ __forceinline__ int page_of(PageRow& r, int key) {
   return __builtin_amdgcn_readlane(r.held, i - r.base);
 }
 __device__ __forceinline__ uint4 signed_query(const uint4& q, uint32_t flip) { return make_uint4(q.x ^ flip, q.y ^ flip, q.z ^ flip, q.w ^ flip); }
-// What the exponents of a column's weights are taken from, whose greatest score is `top` (times log2(e)): `below` less than it in fp16.  Not from 2^23 on, where the
+// What the exponents of a column's weights are taken from, whose greatest score is `top`, times `scale`: `below` less than that in fp16.  Not from `far`, 2^23, on, where the
 // base is a whole number and the greatest weight off by as many powers of two as it is rounded by: half a step is 1 from 2^24 on, and fp16 ends at 2^16.
 template <bool BF>
-__device__ __forceinline__ float weights_base(float top, float below) {
-  return !BF && fabsf(top) < 0x1p23f ? top - below : top;
+__device__ __forceinline__ float weights_base(float top, float scale, float far, float below) {
+  return __builtin_fmaf(top, scale, !BF && fabsf(top) < far ? -below : 0.0f);
 }
 // Greatest value / sum over the lanes of a column, l % 16 (Q16) or l % 32.
 template <bool Q16>
