@@ -331,6 +331,128 @@ int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_by
                    const gear_page_rows* q, int32_t H_q, float scale, const gear_page_rows* out, void* workspace,
                    size_t workspace_bytes, void* stream);
 
+/*
+ * ---- Rotary positions ---------------------------------------------------------------------------
+ * Channels 0 .. rot_dim - 1 of a row at position t are turned pair by pair, the others stay as they are:
+ *     y_a = f (x_a cos(t w_p) - x_b sin(t w_p)),   y_b = f (x_a sin(t w_p) + x_b cos(t w_p)),
+ * pair p < rot_dim / 2 being channels a = p, b = p + rot_dim / 2, or a = 2 p, b = 2 p + 1 (interleaved).  Angles are formed and
+ * reduced in 64 bits (|t w_p| below 2^31: the cosine and sine are off by less than 2^-20, and 2^-22 below 2^24), the turn is fp32, rounded once.
+ */
+typedef struct gear_rope {
+  int32_t rot_dim;       /* even, 2..128                                                          */
+  int32_t interleaved;   /* which channels are a pair: 0 or 1                                     */
+  int32_t inverse;       /* 1: by -t w_p, which takes a turn back (and, times f, is its gradient) */
+  float factor;          /* f, finite; 1 in the plain form                                        */
+  const double* freq;    /* device [rot_dim / 2]: w_p in radians per position                     */
+} gear_rope;
+
+/* How the frequencies base^(-2 p / rot_dim) are brought to longer contexts. */
+typedef enum gear_rope_scaling {
+  GEAR_ROPE_PLAIN = 0,    /* not at all                                                                                */
+  GEAR_ROPE_LINEAR = 1,   /* w / scale (positions interpolated)                                                        */
+  GEAR_ROPE_BASE = 2,     /* base * scale^(rot_dim / (rot_dim - 2)) in place of base: the slowest pair is w / scale    */
+  GEAR_ROPE_TURNS = 3     /* by the turns u = trained_len * w / (2 pi) a pair makes over the trained length: w / scale  */
+                          /* up to `low` turns, w from `high` on, and w (k + (1 - k) / scale), k = (u - low) / (high - low) */
+                          /* between (the ramp of YaRN, whose f is 0.1 ln(scale) + 1)                                  */
+} gear_rope_scaling;
+
+/* Fills host freq [rot_dim / 2].  base and scale are above 0; trained_len, low and high (0 <= low < high) count for GEAR_ROPE_TURNS only. */
+int gear_rope_freq(int scaling, int32_t rot_dim, double base, double scale, double trained_len, double low, double high, double* freq);
+
+/* Turns rows [n_seqs][n_rows][heads][128] of x into out; row (s, t) stands at positions[s * n_rows + t].
+ * dtype     : a gear_dtype.
+ * out       : the same rows as x (in place), or rows that do not overlap them.
+ * positions : device int64, any sign. */
+int gear_rotate(const gear_rope* rope, int dtype, const gear_page_rows* x, const gear_page_rows* out, int32_t n_seqs, int32_t n_rows,
+                int32_t heads, const int64_t* positions, void* stream);
+
+/* A step's rows into the cache in one launch: gear_rotate of q (H_q heads, into q_out) and K, rounded to the cache's type, and gear_page_write of
+ * the turned K and of V, bit for bit.  Queries are turned whatever their row's slot is.
+ * q, q_out  : NULL both (and H_q 0) where only K and V are given; in place as in gear_rotate. */
+int gear_page_write_rope(const gear_page_config* cfg, void* pool, size_t pool_bytes, const gear_rope* rope, const gear_page_rows* K,
+                         const gear_page_rows* V, const gear_page_rows* q, const gear_page_rows* q_out, int32_t H_q, int32_t n_seqs,
+                         int32_t n_rows, const int64_t* slots, const int64_t* positions, void* stream);
+
+/*
+ * ---- Page tables --------------------------------------------------------------------------------
+ * Which pages a sequence has, kept on the device: a step that takes pages, forks sequences or drops tokens needs no host in between and can be
+ * captured.  One table serves all layers, whose pools have the same pages.  A table begins with every entry -1 and every kv_len and count
+ * 0, and is changed by these calls only; then refs[p] is the number of entries that name page p, and entries from ceil(kv_len / page_size) on
+ * are -1.  Results do not depend on the order in which the device works: pages are taken lowest number first, in the order of the list.
+ * Rows outside 0 .. n_rows - 1 in a list are passed over.  The calls on one table must be ordered on one stream.
+ */
+typedef struct gear_page_table {
+  int32_t n_pages;     /* pages of a pool, 1 .. 2^27                       */
+  int32_t page_size;   /* tokens per page: 16, 32, 64, 128 or 256          */
+  int32_t n_rows;      /* sequences, 1 .. 2^18                             */
+  int32_t width;       /* entries of a row, width * page_size below 2^31   */
+  int32_t* table;      /* device [n_rows][width]                           */
+  int32_t* kv_len;     /* device [n_rows]                                  */
+  int32_t* refs;       /* device [n_pages], 16-byte aligned                */
+} gear_page_table;
+
+#define GEAR_PAGE_LIST_MAX 1024   /* entries of a list of rows */
+
+/*
+ * Room for counts[i] more tokens of row rows[i], i = 0 .. n - 1 one after the other: pages are taken for them, and where the first of them
+ * goes into a partly filled page that other entries name, too, the row gets a page of its own in its place.
+ * max_count : columns of slots; a row that asks for more is refused.
+ * slots     : device int64 [n][max_count]: the new tokens' slots, as gear_page_write takes them; -1 behind a row's last.
+ * copies    : device int32 [n][2]: (page, the page in its place), as gear_page_move takes them, or (-1, -1).
+ * refused   : device int32 [n]: 0; 1 where the row is none, is named before in the list, has no room in its width, or the count is
+ *             negative or above max_count; 2 where too few pages are free for it (what those before it asked for counts as taken), or
+ *             where it would have had a shared page to itself if one before it had not been refused a page in its place.  A refused row is left as
+ *             it is, its slots are -1.
+ */
+int gear_page_extend(const gear_page_table* t, const int32_t* rows, const int32_t* counts, int32_t n, int32_t max_count, int64_t* slots,
+                     int32_t* copies, int32_t* refused, void* stream);
+
+/* Row rows[i] keeps its first lens[i] tokens (0: the row is freed); pages that no entry names any more are free.  A row that has fewer is left
+ * as it is; one that is named twice keeps the fewer. */
+int gear_page_truncate(const gear_page_table* t, const int32_t* rows, const int32_t* lens, int32_t n, void* stream);
+
+/* Row dst[i] becomes what row src[i] was before the call, i = 0 .. n - 1: parallel samples of a prompt, beams in another order.  What dst[i]
+ * held is dropped.  A row that is named twice in dst gets the first of its sources. */
+int gear_page_fork(const gear_page_table* t, const int32_t* src, const int32_t* dst, int32_t n, void* stream);
+
+/* The highest pages in use change to the lowest free numbers, until those in use are the first ones or max_moves have moved.
+ * moves  : device int32 [max_moves][2]: (from, to) for gear_page_move, from falling, to rising; (-1, -1) behind the last.
+ * counts : device int32 [2]: pages in use, moves. */
+int gear_page_compact(const gear_page_table* t, int32_t* moves, int32_t max_moves, int32_t* counts, void* stream);
+
+/* Copies page pairs[i][0] over page pairs[i][1] in each of n_pools pools, which lie pool_stride bytes (a multiple of 16) apart.  Pairs with a page
+ * outside 0 .. n_pages - 1 are passed over.  A page that is written should be written once and not be read by another pair: of one that
+ * is, the bytes may come from either, or be those of before or after.
+ * pool_bytes : from `pool` to the end of the last. */
+int gear_page_move(const gear_page_config* cfg, void* pool, size_t pool_bytes, int32_t n_pools, size_t pool_stride, const int32_t* pairs,
+                   int32_t n, void* stream);
+
+/*
+ * ---- Attention with shared prefixes -------------------------------------------------------------
+ * gear_page_attn for a batch whose sequences share their first tokens in groups: samples of one prompt, requests behind one system
+ * prompt, questions about one document.  The shared tokens' pages are read once for all new tokens of a group, instead of once for each sequence, and the two
+ * parts of a row's softmax are joined.  The same batch, and up to the order of sums the same result, as gear_page_attn.
+ */
+typedef struct gear_page_groups {
+  int32_t n_groups;
+  int32_t max_q;                /* no group has more rows of q (the rows of one that has may stay)     */
+  int32_t max_prefix;           /* about the longest prefix: what the work is divided by               */
+  const int32_t* group_start;   /* device [n_groups + 1], ascending: group i has sequences group_start[i] .. */
+  const int32_t* prefix_len;    /* device [n_groups]: the first tokens that are the same in all of them; they are read through the
+                                 * group's first sequence's row of the page table.  Where the sequences part within a page, each may have its own copy. */
+} gear_page_groups;
+
+/* Workspace of gear_page_attn_shared for H_q query heads and every batch and groups with at most these n_seqs, n_tokens, max_q and max_kv, n_groups, max_q and
+ * max_prefix (it serves gear_page_attn for them, too).  Only the int fields are read. */
+int gear_page_attn_shared_bytes(const gear_page_config* cfg, int32_t H_q, const gear_page_batch* batch, const gear_page_groups* groups,
+                                size_t* workspace_bytes);
+
+/* Sequences outside every group share nothing.  A prefix counts as far as all rows of its group's new tokens see it.  The other arguments are
+ * those of gear_page_attn. */
+int gear_page_attn_shared(const gear_page_config* cfg, const void* pool, size_t pool_bytes, const gear_page_batch* batch,
+                          const gear_page_groups* groups, const gear_page_rows* q, int32_t H_q, float scale, const gear_page_rows* out,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
 const char* gear_strerror(int status);
 
 #ifdef __cplusplus

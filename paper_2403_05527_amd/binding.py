@@ -17,6 +17,9 @@ EXPORTED = [
     "gear_cache_bytes", "gear_cache_init", "gear_cache_reset", "gear_compress", "gear_compress_recent", "gear_decompress",
     "gear_decode_attn", "gear_decode_attn_mq", "gear_decode_attn_static", "gear_export_codes", "gear_export_sparse", "gear_export_sparse_coo", "gear_export_lowrank", "gear_strerror",
     "gear_page_bytes", "gear_page_write", "gear_page_read", "gear_page_attn_bytes", "gear_page_attn",
+    "gear_rope_freq", "gear_rotate", "gear_page_write_rope",
+    "gear_page_extend", "gear_page_truncate", "gear_page_fork", "gear_page_compact", "gear_page_move",
+    "gear_page_attn_shared_bytes", "gear_page_attn_shared",
 ]
 
 
@@ -53,6 +56,20 @@ class gear_page_batch(ctypes.Structure):
                [(n, ctypes.c_void_p) for n in ("q_start", "kv_len", "page_table")]
 
 
+class gear_rope(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rot_dim", "interleaved", "inverse")] + [("factor", ctypes.c_float), ("freq", ctypes.c_void_p)]
+
+
+class gear_page_table(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "n_rows", "width")] + [(n, ctypes.c_void_p) for n in ("table", "kv_len", "refs")]
+
+
+class gear_page_groups(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_groups", "max_q", "max_prefix")] + [(n, ctypes.c_void_p) for n in ("group_start", "prefix_len")]
+
+
+GEAR_PAGE_LIST_MAX = 1024
+GEAR_ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "turns": 3}
 GEAR_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
 
 
@@ -94,6 +111,17 @@ def load_library():
     lib.gear_page_read.argtypes = [pcfg, vp, sz, rows, rows, i32, i32, vp, vp]
     lib.gear_page_attn_bytes.argtypes = [pcfg, i32, batch, ctypes.POINTER(sz)]
     lib.gear_page_attn.argtypes = [pcfg, vp, sz, batch, rows, i32, ctypes.c_float, rows, vp, sz, vp]
+    rope, table, groups, f64 = ctypes.POINTER(gear_rope), ctypes.POINTER(gear_page_table), ctypes.POINTER(gear_page_groups), ctypes.c_double
+    lib.gear_rope_freq.argtypes = [ctypes.c_int, i32, f64, f64, f64, f64, f64, ctypes.POINTER(f64)]
+    lib.gear_rotate.argtypes = [rope, ctypes.c_int, rows, rows, i32, i32, i32, vp, vp]
+    lib.gear_page_write_rope.argtypes = [pcfg, vp, sz, rope, rows, rows, rows, rows, i32, i32, i32, vp, vp, vp]
+    lib.gear_page_extend.argtypes = [table, vp, vp, i32, i32, vp, vp, vp, vp]
+    lib.gear_page_truncate.argtypes = [table, vp, vp, i32, vp]
+    lib.gear_page_fork.argtypes = [table, vp, vp, i32, vp]
+    lib.gear_page_compact.argtypes = [table, vp, i32, vp, vp]
+    lib.gear_page_move.argtypes = [pcfg, vp, sz, i32, sz, vp, i32, vp]
+    lib.gear_page_attn_shared_bytes.argtypes = [pcfg, i32, batch, groups, ctypes.POINTER(sz)]
+    lib.gear_page_attn_shared.argtypes = [pcfg, vp, sz, batch, groups, rows, i32, ctypes.c_float, rows, vp, sz, vp]
     lib.gear_strerror.argtypes = [ctypes.c_int]
     lib.gear_strerror.restype = ctypes.c_char_p
     for name in EXPORTED:
@@ -310,7 +338,7 @@ def gear_page_attn_bytes(cfg, H_q, batch):
     return n.value
 
 
-def gear_page_attn(cfg, pool, batch, q, out, scale, workspace):
+def _attn_arguments(cfg, pool, batch, q, out, workspace):
     device = _page_device()
     if getattr(batch, "device", device) != device:
         raise ValueError("the batch's lengths and page table lie on cuda:%d, not on the current GPU" % batch.device)
@@ -321,7 +349,163 @@ def gear_page_attn(cfg, pool, batch, q, out, scale, workspace):
         raise ValueError("q and out are [%d, H_q, %d]: got %s and %s" % (batch.n_tokens, cfg.d_h, tuple(q.shape), tuple(out.shape)))
     p, size = _page_bytes(pool, device, "the pool")
     w, w_size = (None, 0) if workspace is None else _page_bytes(workspace, device, "the workspace")
+    return p, size, a, b, H_q, w, w_size
+
+
+def gear_page_attn(cfg, pool, batch, q, out, scale, workspace):
+    p, size, a, b, H_q, w, w_size = _attn_arguments(cfg, pool, batch, q, out, workspace)
     _check(load_library().gear_page_attn(cfg, p, size, batch, a, H_q, scale, b, w, w_size, _stream()), "gear_page_attn")
+
+
+# ---- rotary positions
+class _RowsOf(ctypes.Structure):   # what _page_rows asks of a configuration
+    _fields_ = [("d_h", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+def gear_rope_freq(rot_dim=128, base=10000.0, scaling="plain", scale=1.0, trained_len=0.0, low=1.0, high=4.0):
+    """The frequencies as a float64 tensor on the host, radians per position and pair."""
+    freq = torch.empty(max(0, rot_dim // 2), dtype=torch.float64)
+    _check(load_library().gear_rope_freq(GEAR_ROPE_SCALINGS[scaling], rot_dim, base, scale, trained_len, low, high,
+                                         ctypes.cast(freq.data_ptr(), ctypes.POINTER(ctypes.c_double))), "gear_rope_freq")
+    return freq
+
+
+def make_rope(freq, interleaved=False, inverse=False, factor=1.0):
+    """The rotation of one model's rows (one serves all layers): float64 frequencies on the GPU, which it keeps alive."""
+    d = _page_device()
+    r = gear_rope(2 * freq.numel(), 1 if interleaved else 0, 1 if inverse else 0, factor, _page_index(freq, torch.float64, freq.numel(), d, "freq"))
+    r.tensors, r.device = freq, d
+    return r
+
+
+def _rope_device(rope, device):
+    if getattr(rope, "device", device) != device:
+        raise ValueError("the frequencies lie on cuda:%d, not on the current GPU" % rope.device)
+
+
+def gear_rotate(rope, x, out, positions):
+    """x, out: [n_seqs, tokens, heads, 128], or without the first; out may be x."""
+    device = _page_device()
+    _rope_device(rope, device)
+    if x.dtype not in GEAR_DTYPES or x.shape != out.shape:
+        raise ValueError("x and out are fp16 or bf16 rows of one shape: got %s %s and %s" % (x.dtype, tuple(x.shape), tuple(out.shape)))
+    kind, heads = _RowsOf(128, GEAR_DTYPES[x.dtype]), x.shape[-2] if x.dim() > 1 else 0
+    a, n_seqs, n_rows = _page_rows(x, kind, heads, device, "x")
+    b = _page_rows(out, kind, heads, device, "out")[0]
+    _check(load_library().gear_rotate(rope, kind.dtype, a, b, n_seqs, n_rows, heads,
+                                      _page_index(positions, torch.int64, n_seqs * n_rows, device, "positions"), _stream()), "gear_rotate")
+
+
+def gear_page_write_rope(cfg, pool, rope, K, V, slots, positions, q=None, q_out=None):
+    device = _page_device()
+    _rope_device(rope, device)
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out come together")
+    k, n_seqs, n_rows = _page_rows(K, cfg, cfg.H_kv, device, "K")
+    v = _page_rows(V, cfg, cfg.H_kv, device, "V")
+    if v[1:] != (n_seqs, n_rows):
+        raise ValueError("K and V differ in their rows: %s and %s" % (tuple(K.shape), tuple(V.shape)))
+    a = b = None
+    H_q = 0
+    if q is not None:
+        H_q = q.shape[-2]
+        a, b = _page_rows(q, cfg, H_q, device, "q"), _page_rows(q_out, cfg, H_q, device, "q_out")
+        if not H_q or a[1:] != (n_seqs, n_rows) or b[1:] != (n_seqs, n_rows):
+            raise ValueError("q, q_out and K differ in their rows: %s, %s and %s" % (tuple(q.shape), tuple(q_out.shape), tuple(K.shape)))
+    p, size = _page_bytes(pool, device, "the pool")
+    n = n_seqs * n_rows
+    _check(load_library().gear_page_write_rope(cfg, p, size, rope, k, v[0], a and a[0], b and b[0], H_q, n_seqs, n_rows,
+                                               _page_index(slots, torch.int64, n, device, "slots"),
+                                               _page_index(positions, torch.int64, n, device, "positions"), _stream()), "gear_page_write_rope")
+
+
+# ---- page tables
+def make_page_table(table, kv_len, refs, page_size):
+    """int32 tensors table [n_rows, width], kv_len [n_rows], refs [n_pages], which it keeps alive."""
+    n_rows, width = table.shape
+    d = _page_device()
+    t = gear_page_table(refs.numel(), page_size, n_rows, width, _page_index(table, torch.int32, n_rows * width, d, "table"),
+                        _page_index(kv_len, torch.int32, n_rows, d, "kv_len"), _page_index(refs, torch.int32, refs.numel(), d, "refs"))
+    t.tensors, t.device = (table, kv_len, refs), d
+    return t
+
+
+def _table_lists(t, *lists):
+    """(addresses, entries) of int32 lists of one length."""
+    device = _page_device()
+    if getattr(t, "device", device) != device:
+        raise ValueError("the page table lies on cuda:%d, not on the current GPU" % t.device)
+    n = lists[0][0].numel()
+    return [_page_index(x, torch.int32, n * per, device, what) for x, per, what in lists], n
+
+
+def gear_page_extend(t, rows, counts, slots, copies, refused):
+    """slots: int64 [n, max_count]; copies int32 [n, 2]; refused int32 [n]."""
+    (r, c, p, f), n = _table_lists(t, (rows, 1, "rows"), (counts, 1, "counts"), (copies, 2, "copies"), (refused, 1, "refused"))
+    if slots.dim() != 2 or slots.shape[0] != n:
+        raise ValueError("slots is [%d, max_count]: got %s" % (n, tuple(slots.shape)))
+    _check(load_library().gear_page_extend(t, r, c, n, slots.shape[1], _page_index(slots, torch.int64, slots.numel(), _page_device(), "slots"), p, f, _stream()),
+           "gear_page_extend")
+
+
+def gear_page_truncate(t, rows, lens):
+    (r, k), n = _table_lists(t, (rows, 1, "rows"), (lens, 1, "lens"))
+    _check(load_library().gear_page_truncate(t, r, k, n, _stream()), "gear_page_truncate")
+
+
+def gear_page_fork(t, src, dst):
+    (a, b), n = _table_lists(t, (src, 1, "src"), (dst, 1, "dst"))
+    _check(load_library().gear_page_fork(t, a, b, n, _stream()), "gear_page_fork")
+
+
+def gear_page_compact(t, moves, counts):
+    """moves: int32 [max_moves, 2]; counts int32 [2]: pages in use, moves."""
+    if moves.dim() != 2 or moves.shape[1] != 2:
+        raise ValueError("moves is [max_moves, 2]: got %s" % (tuple(moves.shape),))
+    (c,), _ = _table_lists(t, (counts, 1, "counts"))
+    if counts.numel() != 2:
+        raise ValueError("counts has two entries: got %s" % (tuple(counts.shape),))
+    _check(load_library().gear_page_compact(t, _page_index(moves, torch.int32, moves.numel(), _page_device(), "moves"), moves.shape[0], c, _stream()),
+           "gear_page_compact")
+
+
+def gear_page_move(cfg, pool, pairs):
+    """pool: the bytes of one pool, or [n_pools, bytes] with rows of one stride (a layer's pool each); pairs: int32 [n, 2]."""
+    device = _page_device()
+    if pool.get_device() != device or pool.dim() not in (1, 2) or pool.stride(-1) != 1:
+        raise ValueError("the pool is contiguous bytes on the current GPU, or rows of them: got %s on %s" % (tuple(pool.shape), pool.device))
+    if pairs.dim() != 2 or pairs.shape[1] != 2:
+        raise ValueError("pairs is [n, 2]: got %s" % (tuple(pairs.shape),))
+    es = pool.element_size()
+    n_pools, stride = (1, 0) if pool.dim() == 1 else (pool.shape[0], pool.stride(0) * es)
+    size = pool.shape[-1] * es + max(0, n_pools - 1) * stride
+    _check(load_library().gear_page_move(cfg, pool.data_ptr(), size, n_pools, stride, _page_index(pairs, torch.int32, pairs.numel(), device, "pairs"),
+                                         pairs.shape[0], _stream()), "gear_page_move")
+
+
+# ---- attention with shared prefixes
+def make_page_groups(group_start, prefix_len, max_q, max_prefix):
+    """The groups of a batch: int32 tensors group_start [n_groups + 1], prefix_len [n_groups], which it keeps alive."""
+    n = prefix_len.numel()
+    d = _page_device()
+    g = gear_page_groups(n, max_q, max_prefix, _page_index(group_start, torch.int32, n + 1, d, "group_start"),
+                         _page_index(prefix_len, torch.int32, n, d, "prefix_len"))
+    g.tensors, g.device = (group_start, prefix_len), d
+    return g
+
+
+def gear_page_attn_shared_bytes(cfg, H_q, batch, groups):
+    n = ctypes.c_size_t(0)
+    _check(load_library().gear_page_attn_shared_bytes(ctypes.byref(cfg), H_q, ctypes.byref(batch), ctypes.byref(groups), ctypes.byref(n)),
+           "gear_page_attn_shared_bytes")
+    return n.value
+
+
+def gear_page_attn_shared(cfg, pool, batch, groups, q, out, scale, workspace):
+    p, size, a, b, H_q, w, w_size = _attn_arguments(cfg, pool, batch, q, out, workspace)
+    if getattr(groups, "device", _page_device()) != _page_device():
+        raise ValueError("the groups lie on cuda:%d, not on the current GPU" % groups.device)
+    _check(load_library().gear_page_attn_shared(cfg, p, size, batch, groups, a, H_q, scale, b, w, w_size, _stream()), "gear_page_attn_shared")
 
 
 # ---- convenience owner of the device buffers -------------------------------
@@ -428,6 +612,16 @@ class PagePool:
     def write(self, K, V, slots):
         gear_page_write(self.cfg, self.pool, K, V, slots)
 
+    def write_rope(self, rope, K, V, slots, positions, q=None, q_out=None):
+        """Turned Keys and Values into their slots; the turned queries, if there are any."""
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        gear_page_write_rope(self.cfg, self.pool, rope, K, V, slots, positions, q, q_out)
+        return q_out
+
+    def move(self, pairs):
+        gear_page_move(self.cfg, self.pool, pairs)
+
     def read(self, slots, heads_first=False):
         """K, V of slots [n_seqs, tokens] as [n_seqs, tokens, H_kv, 128], or [n_seqs, H_kv, tokens, 128]: what GearCache.compress takes.
         Rows whose slot is outside the pool are 0."""
@@ -450,3 +644,46 @@ class PagePool:
             workspace = self.workspace_for(q.shape[-2], batch)
         gear_page_attn(self.cfg, self.pool, batch, q, out, self.cfg.d_h ** -0.5 if scale is None else scale, workspace)
         return out
+
+    def attn_shared(self, q, batch, groups, scale=None, out=None, workspace=None):
+        if out is None:
+            out = torch.empty_like(q)
+        if workspace is None:
+            n = gear_page_attn_shared_bytes(self.cfg, q.shape[-2], batch, groups)
+            workspace = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+        gear_page_attn_shared(self.cfg, self.pool, batch, groups, q, out, self.cfg.d_h ** -0.5 if scale is None else scale, workspace)
+        return out
+
+
+class PageTable:
+    """Allocates a page table; forwards to the C ABI.  One serves the pools of all layers."""
+
+    def __init__(self, n_pages, page_size, n_rows, width, device="cuda:0"):
+        self.device = torch.device(device)
+        self.page_size = page_size
+        self.table = torch.full((n_rows, width), -1, dtype=torch.int32, device=self.device)
+        self.kv_len = torch.zeros(n_rows, dtype=torch.int32, device=self.device)
+        self.refs = torch.zeros(n_pages, dtype=torch.int32, device=self.device)
+        self.c = make_page_table(self.table, self.kv_len, self.refs, page_size)
+
+    def _new(self, *shape, dtype=torch.int32):
+        return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def extend(self, rows, counts, max_count):
+        """(slots [n, max_count], copies [n, 2], refused [n]) of counts[i] more tokens in row rows[i]."""
+        n = rows.numel()
+        slots, copies, refused = self._new(n, max_count, dtype=torch.int64), self._new(n, 2), self._new(n)
+        gear_page_extend(self.c, rows, counts, slots, copies, refused)
+        return slots, copies, refused
+
+    def truncate(self, rows, lens):
+        gear_page_truncate(self.c, rows, lens)
+
+    def fork(self, src, dst):
+        gear_page_fork(self.c, src, dst)
+
+    def compact(self, max_moves):
+        """(moves [max_moves, 2], counts [2]: pages in use, moves)."""
+        moves, counts = self._new(max_moves, 2), self._new(2)
+        gear_page_compact(self.c, moves, counts)
+        return moves, counts

@@ -12,16 +12,18 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libgear.so")
 
 CSRC_PAGES = os.path.join(PKG, "csrc_pages")   # the paged cache
+CSRC_SERVING = os.path.join(PKG, "csrc_serving")   # rotary positions, page tables, shared prefixes
 
 SOURCES = [os.path.join(CSRC, s) for s in ("gear_api.hip", "compress_filter.hip", "compress_values.hip", "lowrank.hip", "decode.hip",
                                            "decompress_export.hip")]
 SOURCES += [os.path.join(CSRC_PAGES, s) for s in ("page_api.hip", "page_copy.hip", "page_few.hip", "page_many.hip", "page_mixed.hip")]
+SOURCES += [os.path.join(CSRC_SERVING, s) for s in ("rope_api.hip", "rope.hip", "table_api.hip", "table.hip", "shared_api.hip", "shared.hip")]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wno-unused-command-line-argument", "-Wno-unknown-warning-option",
-    "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-I", CSRC_PAGES,
+    "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-I", CSRC_PAGES, "-I", CSRC_SERVING,
 ]
 
 

@@ -1,18 +1,9 @@
 // Entry points of the paged cache (include/gear.h): arguments are checked here, before anything is launched.
 #include <cmath>
+#include "page_checks.h"
 #include "page_launch.h"
 
 namespace gear {
-
-constexpr size_t RECORD_BYTES = (2 + D) * sizeof(float);   // of one column and part
-#ifndef GEAR_PAGE_CUS   // (the CPU stand-in sets it, so that its small cases are divided)
-#define GEAR_PAGE_CUS GEAR_CUS
-#endif
-constexpr int FEW_COLS_MOST = 32;
-// Blocks of either kernel that the chip holds at once (of few columns: with one tile of them, with two half as many), and the most that dividing the
-// keys makes of fewer: they bound the records, 64 MB of both kinds.
-constexpr int FEW_SLOTS = 2 * GEAR_PAGE_CUS, MANY_SLOTS = 2 * GEAR_PAGE_CUS;
-constexpr int FEW_BLOCKS_MOST = FEW_SLOTS * 3 / 2, MANY_BLOCKS_MOST = MANY_SLOTS * 3 / 2;
 
 // The number of equal parts of the key axis that a model finds the fastest, in ns: `blocks` of them undivided on `slots` places, each taking `once` and 2 us
 // per `step` tokens, begun or whole; all together no less than `bytes` (the memory's share); with more than one part, a merge whose records (`records` bytes
@@ -20,7 +11,7 @@ constexpr int FEW_BLOCKS_MOST = FEW_SLOTS * 3 / 2, MANY_BLOCKS_MOST = MANY_SLOTS
 // crowded: what a block's time is multiplied by where there are more than CUs (the last to end shares its CU); `merges`: the blocks of the merge, 2.2 ns each.
 // filled: parts have a length, not a number, so sequences shorter than max_kv make fewer; but no more than 86 % of the slots count, since blocks that end at once
 // leave the XCDs unevenly filled (504 parts on 512 slots: the last dozen began when the first had ended).
-static int best_parts(int64_t blocks, double filled, int slots, int most_blocks, int max_kv, int least_part, double once, int step, double crowded, double bytes,
+int best_parts(int64_t blocks, double filled, int slots, int most_blocks, int max_kv, int least_part, double once, int step, double crowded, double bytes,
                       double records, double merges) {
   const int64_t by_blocks = blocks > 0 ? most_blocks / blocks : 1;
   const int by_keys = max_kv / least_part, most = (int)(by_blocks < by_keys ? by_blocks : by_keys);
@@ -103,64 +94,6 @@ using namespace gear;
 
 namespace {
 
-constexpr int64_t INT_MOST = 0x7FFFFFFF, THREADS_MOST = 0xFFFFFFFF;   // of a launch
-
-int check_page_config(const gear_page_config* c, size_t* pool_bytes, PageGeom* g) {
-  if (!c) return GEAR_EINVAL;
-  if (c->d_h != D || c->n_pages < 1 || c->H_kv < 1 || c->H_kv > 1024) return GEAR_EINVAL;
-  if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1))) return GEAR_EINVAL;
-  if (c->bits != 16 && c->bits != 8 && c->bits != 4) return GEAR_EINVAL;
-  if (c->bits != 16 && c->group != 32 && c->group != 64 && c->group != 128) return GEAR_EINVAL;
-  if (c->dtype != GEAR_F16 && c->dtype != GEAR_BF16) return GEAR_EINVAL;
-  const int group = c->bits == 16 ? D : c->group;
-  g->row_bytes = (uint32_t)(D * c->bits / 8);
-  g->block_bytes = (uint32_t)c->page_size * (g->row_bytes + (c->bits == 16 ? 0u : 4u * (uint32_t)(D / group)));
-  g->page_bytes = 2ull * (uint64_t)c->H_kv * g->block_bytes;
-  g->n_pages = c->n_pages;
-  g->shift = __builtin_ctz((unsigned)c->page_size);
-  g->gshift = __builtin_ctz((unsigned)group);
-  g->H = c->H_kv;
-  g->pool = nullptr;
-  if (g->page_bytes >= (1ull << 31)) return GEAR_ECAPACITY;
-  *pool_bytes = (size_t)g->page_bytes * (size_t)c->n_pages;
-  return GEAR_OK;
-}
-
-bool misaligned(const void* p, uintptr_t by) { return (reinterpret_cast<uintptr_t>(p) & (by - 1)) != 0; }
-
-int check_pool(const gear_page_config* cfg, const void* pool, size_t pool_bytes, PageGeom* g) {
-  size_t need = 0;
-  const int rc = check_page_config(cfg, &need, g);
-  if (rc) return rc;
-  if (!pool) return GEAR_EINVAL;
-  if (misaligned(pool, 16)) return GEAR_EALIGN;
-  if (pool_bytes < need) return GEAR_ECAPACITY;
-  g->pool = static_cast<const unsigned char*>(pool);
-  return GEAR_OK;
-}
-
-// Whether rows of these strides lie over one another: within one direction, or one step of two directions in the same place.  (Whatever is laid out one direction
-// after the other does not; strides that overlap in other ways are the caller's.)
-bool rows_overlap(int64_t n_seqs, int64_t seq, int64_t n_rows, int64_t token, int64_t heads, int64_t head) {
-  const int64_t count[3] = {n_seqs, n_rows, heads}, stride[3] = {seq, token, head};
-  for (int i = 0; i < 3; ++i) {
-    if (count[i] <= 1) continue;
-    if (stride[i] < D && stride[i] > -D) return true;
-    for (int j = 0; j < i; ++j)
-      if (count[j] > 1 && (stride[i] == stride[j] || stride[i] == -stride[j])) return true;
-  }
-  return false;
-}
-int check_rows(const gear_page_rows* r, int64_t n_seqs, int64_t n_rows, int64_t heads, bool written) {
-  if (!r->data) return GEAR_EINVAL;
-  if (misaligned(r->data, 16) || (n_seqs > 1 && r->seq % 8) || (n_rows > 1 && r->token % 8) || (heads > 1 && r->head % 8)) return GEAR_EALIGN;
-  if (written && rows_overlap(n_seqs, r->seq, n_rows, r->token, heads, r->head)) return GEAR_EINVAL;
-  return GEAR_OK;
-}
-RowView view_of(const gear_page_rows* r) {
-  return r ? RowView{static_cast<unsigned char*>(r->data), r->seq, r->token, r->head} : RowView{nullptr, 0, 0, 0};
-}
-
 int copy_rows(const gear_page_config* cfg, const void* pool, size_t pool_bytes, const gear_page_rows* K, const gear_page_rows* V,
               int32_t n_seqs, int32_t n_rows, const int64_t* slots, bool write, void* stream) {
   PageGeom g;
@@ -177,15 +110,6 @@ int copy_rows(const gear_page_config* cfg, const void* pool, size_t pool_bytes, 
   if (total > INT_MOST - 4096 || chunks * cfg->H_kv > THREADS_MOST / 256) return GEAR_ECAPACITY;
   return launch_page_copy(g, cfg->bits, cfg->dtype == GEAR_BF16, write, view_of(K), view_of(V), slots, n_seqs, n_rows,
                           static_cast<hipStream_t>(stream)) == hipSuccess ? GEAR_OK : GEAR_EHIP;
-}
-
-int check_batch(const gear_page_config* cfg, int32_t H_q, const gear_page_batch* b) {
-  if (!b || H_q < 1 || H_q % cfg->H_kv) return GEAR_EINVAL;
-  if (b->n_seqs < 0 || b->n_tokens < 0 || b->max_q < 0 || b->max_kv < 0) return GEAR_EINVAL;
-  // (all indices of columns, blocks and records' rows are 32-bit numbers)
-  if ((int64_t)b->n_tokens * H_q > INT_MOST || (int64_t)b->max_q * H_q > INT_MOST) return GEAR_ECAPACITY;
-  if ((int64_t)b->n_seqs * H_q * FEW_COLS_MOST > INT_MOST) return GEAR_ECAPACITY;
-  return GEAR_OK;
 }
 
 }  // namespace
@@ -225,16 +149,10 @@ int gear_page_attn_bytes(const gear_page_config* cfg, int32_t H_q, const gear_pa
 int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_bytes, const gear_page_batch* batch, const gear_page_rows* q,
                    int32_t H_q, float scale, const gear_page_rows* out, void* workspace, size_t workspace_bytes, void* stream) {
   PageAttn a{};
-  int rc = check_pool(cfg, pool, pool_bytes, &a.geom);
-  if (rc || (rc = check_batch(cfg, H_q, batch))) return rc;
+  const int rc = check_attn(cfg, pool, pool_bytes, batch, q, H_q, scale, out, workspace, &a);
+  if (rc) return rc;
   const gear_page_batch& b = *batch;
-  const float scale_log2 = std::fabs(scale) * 1.44269504088896340736f;
-  if (!q || !out || !std::isfinite(scale_log2) || b.table_width < 0) return GEAR_EINVAL;
   if (b.n_seqs == 0 || b.n_tokens == 0 || b.max_q == 0) return GEAR_OK;
-  if ((rc = check_rows(q, 1, b.n_tokens, H_q, false)) || (rc = check_rows(out, 1, b.n_tokens, H_q, true))) return rc;
-  if (!b.q_start || !b.kv_len || (b.table_width > 0 && !b.page_table)) return GEAR_EINVAL;
-  if (misaligned(b.q_start, 4) || misaligned(b.kv_len, 4) || misaligned(b.page_table, 4) || misaligned(workspace, 16)) return GEAR_EALIGN;
-  if ((int64_t)b.table_width * cfg->page_size > INT_MOST - 1024) return GEAR_ECAPACITY;
   const int H = cfg->H_kv, gq = H_q / H;
   const int per_key = 2 * (int)(a.geom.block_bytes >> a.geom.shift);
   const PagePlan p = page_plan(H, gq, b.n_seqs, b.n_tokens, b.max_q, b.max_kv, per_key);
@@ -246,19 +164,6 @@ int gear_page_attn(const gear_page_config* cfg, const void* pool, size_t pool_by
   const int64_t tiles = (int64_t)b.n_tokens * gq / MANY_COLS + b.n_seqs;
   if ((int64_t)b.n_seqs * H * p.few_split + tiles * H * p.many_split > THREADS_MOST / 512) return GEAR_ECAPACITY;
 
-  a.q_start = b.q_start;
-  a.kv_len = b.kv_len;
-  a.table = b.page_table;
-  a.q = view_of(q);
-  a.out = view_of(out);
-  a.scale_log2 = std::fmax(scale_log2, 1e-37f);   // (a scale of 0: every score comes to less than a step of 2^0)
-  a.far = 0x1p23f / a.scale_log2;
-  a.flip = scale < 0.0f ? 0x80008000u : 0u;
-  a.width = b.table_width;
-  a.n_seqs = b.n_seqs;
-  a.n_tokens = b.n_tokens;
-  a.gq = gq;
-  a.causal = b.causal ? 1 : 0;
   a.few = p.few_limit;
   a.few_cols = p.few_limit;
   a.tiles = (int32_t)tiles;

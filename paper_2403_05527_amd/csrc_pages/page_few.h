@@ -126,20 +126,21 @@ template <int NC, int WAVES>
 constexpr size_t few_lds_bytes() {
   return WAVES * NC * (16 * 2 * 4 + 8 * 64 * 16);
 }
-template <int BITS, bool BF, int NC, int WAVES>
-__device__ __forceinline__ void few_columns(const PageAttn& a, int bid, unsigned char* lds) {
+template <int BITS, bool BF, int NC, int WAVES, class Attn>
+__device__ __forceinline__ void few_columns(const Attn& a, int bid, unsigned char* lds) {
   const PageGeom& g = a.geom;
   const int head = bid % g.H, rest = bid / g.H, part = rest % a.n_split, s = rest / a.n_split;
   const int lane = lane_id(), wave = GEAR_WAVE_UNIFORM((int)(threadIdx.x >> 6)), c = lane & 15, hh = lane >> 4;
-  const SeqSpan sp = seq_span(a, s);
+  const Span span = span_of(a, s);
+  const SeqSpan& sp = span.sp;
   const int cols = sp.nq * a.gq;
   if (sp.nq <= 0 || sp.nq > a.few || cols > a.few) return;
-  const Parts parts = parts_of(sp.kv, a.n_split, a.least, KEY_STEP);
+  const Parts parts = parts_of(sp.kv - span.begin, a.n_split, a.least, KEY_STEP);
   if (part >= parts.count) return;
-  const int k0 = part * parts.len, k1 = min(sp.kv, k0 + parts.len);
+  const int k0 = span.begin + part * parts.len, k1 = min(sp.kv, k0 + parts.len);
 
   // The first pages are requested with the queries and looked at behind them (8.5 -> 8.0 us behind 512).
-  PageRow pages = page_row(a, s, k1);
+  PageRow pages = page_row(a, span.table_row, k1);
   const int first_entry = (k0 + KEY_STEP * wave) >> g.shift;
   const int32_t entry = k1 > 0 ? pages.table[min(first_entry + lane, (k1 - 1) >> g.shift)] : -1;
 
@@ -316,13 +317,13 @@ __device__ __forceinline__ void few_columns(const PageAttn& a, int bid, unsigned
     if (col >= cols) continue;
     const float sum = NC == 1 || n == 0 ? total[0] : total[NC - 1];
     const int ch = 32 * hh + 4 * k;
-    if (parts.count == 1) {
+    const int row = col / a.gq, j = col - row * a.gq;
+    if (is_output(a, span, parts.count)) {
       const float r = sum > 0.0f ? 1.0f / sum : 0.0f;
-      const int row = col / a.gq, j = col - row * a.gq;
       unsigned char* p = a.out.data + 2 * ((int64_t)(sp.q0 + row) * a.out.token + (int64_t)(head * a.gq + j) * a.out.head + ch);
       *reinterpret_cast<uint2*>(p) = make_uint2(pack2<BF>(x.x * r, x.y * r), pack2<BF>(x.z * r, x.w * r));
     } else {
-      const int64_t rec = (((int64_t)s * g.H + head) * a.few_cols + col) * a.n_split + part;
+      const int64_t rec = few_record(a, s, head, col, part, sp.q0 + row, head * a.gq + j);
       *reinterpret_cast<float4*>(a.rec_o + rec * D + ch) = x;
       if (ch == 0) a.rec_ml[rec] = make_float2(NC == 1 || n == 0 ? top[0] : top[NC - 1], sum);
     }

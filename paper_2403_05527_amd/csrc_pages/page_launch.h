@@ -8,6 +8,19 @@ namespace gear {
 hipError_t launch_page_copy(const PageGeom& g, int bits, bool bf, bool write, const RowView& k, const RowView& v, const int64_t* slots,
                             int n_seqs, int n_rows, hipStream_t st);
 
+constexpr size_t RECORD_BYTES = (2 + D) * sizeof(float);   // of one column and part
+#ifndef GEAR_PAGE_CUS   // (the CPU stand-in sets it, so that its small cases are divided)
+#define GEAR_PAGE_CUS GEAR_CUS
+#endif
+constexpr int FEW_COLS_MOST = 32;
+// Blocks of either kernel that the chip holds at once (of few columns: with one tile of them, with two half as many), and the most that dividing the
+// keys makes of fewer: they bound the records, 64 MB of both kinds.
+constexpr int FEW_SLOTS = 2 * GEAR_PAGE_CUS, MANY_SLOTS = 2 * GEAR_PAGE_CUS;
+constexpr int FEW_BLOCKS_MOST = FEW_SLOTS * 3 / 2, MANY_BLOCKS_MOST = MANY_SLOTS * 3 / 2;
+
+int best_parts(int64_t blocks, double filled, int slots, int most_blocks, int max_kv, int least_part, double once, int step, double crowded, double bytes,
+               double records, double merges);
+
 // What a call of gear_page_attn launches: parts of the key axis for sequences of few columns and of many, whether either kind is
 // launched, and the records that the parts leave.
 struct PagePlan {

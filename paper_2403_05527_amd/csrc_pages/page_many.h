@@ -146,8 +146,8 @@ __device__ __forceinline__ ColTile col_tile(const PageAttn& a, int i, int lane) 
 }
 
 // One (column tile, KV head, part) of the call.  lds: [two tiles][Keys, Values][64 rows].  ALONE: no blocks of few columns in the launch.
-template <int BITS, bool BF, bool ALONE>
-__device__ __forceinline__ void many_columns(const PageAttn& a, int bid, unsigned char* lds) {
+template <int BITS, bool BF, bool ALONE, class Attn>
+__device__ __forceinline__ void many_columns(const Attn& a, int bid, unsigned char* lds) {
   const PageGeom& g = a.geom;
   const int lane = lane_id(), wave = GEAR_WAVE_UNIFORM((int)(threadIdx.x >> 6)), c = lane & 31, half = lane >> 5;
   // heads next to each other: with 8 of them and more, a head's tiles share one XCD's L2
@@ -155,13 +155,14 @@ __device__ __forceinline__ void many_columns(const PageAttn& a, int bid, unsigne
   const ColTile ct = col_tile(a, rest / a.n_split, lane);
   if (ct.s < 0) return;
   const int s = ct.s, col0 = ct.col0;
-  const SeqSpan sp = seq_span(a, s);
+  const Span span = span_of(a, s);
+  const SeqSpan& sp = span.sp;
   const int cols = sp.nq * a.gq;
   const int last = min(col0 + MANY_COLS, cols) - 1;
   const int keys = row_sees(a, sp, last / a.gq);
-  const Parts parts = parts_of(keys, a.n_split, a.least, MANY_KEYS);
+  const Parts parts = parts_of(keys - span.begin, a.n_split, a.least, MANY_KEYS);
   if (part >= parts.count) return;
-  const int k0 = part * parts.len, k1 = min(keys, k0 + parts.len);
+  const int k0 = span.begin + part * parts.len, k1 = min(keys, k0 + parts.len);
 
   const int my = col0 + 32 * wave + c, row = my / a.gq, j = my - row * a.gq;
   const bool mine = my < cols, busy = col0 + 32 * wave < cols;   // `busy`: the wave has columns
@@ -176,7 +177,7 @@ __device__ __forceinline__ void many_columns(const PageAttn& a, int bid, unsigne
   }
   const int all_see = row_sees(a, sp, min(col0 + 32 * wave, cols - 1) / a.gq);   // every column of the wave sees the keys before this one
 
-  PageRow pages = page_row(a, s, k1);
+  PageRow pages = page_row(a, span.table_row, k1);
   const Biases bs = biases();
   Staged<BITS> next;                       // codes on their way
   const StageOffsets<BITS> offsets = stage_offsets<BITS>(g, lane);
@@ -316,7 +317,7 @@ __device__ __forceinline__ void many_columns(const PageAttn& a, int bid, unsigne
   if (!mine) return;
   // the lane has channels 32 t + 8 a + 4 half + 0..3 of its column
   const int64_t token = sp.q0 + row;
-  if (parts.count == 1) {
+  if (is_output(a, span, parts.count)) {
     const float r = l > 0.0f ? 1.0f / l : 0.0f;
     unsigned char* p = a.out.data + 2 * (token * a.out.token + (int64_t)(head * a.gq + j) * a.out.head + 4 * half);
 #pragma unroll
@@ -326,7 +327,7 @@ __device__ __forceinline__ void many_columns(const PageAttn& a, int bid, unsigne
         *reinterpret_cast<uint2*>(p + 64 * t + 16 * k) =
             make_uint2(pack2<BF>(o[t][4 * k] * r, o[t][4 * k + 1] * r), pack2<BF>(o[t][4 * k + 2] * r, o[t][4 * k + 3] * r));
   } else {
-    const int64_t rec = (token * ((int64_t)g.H * a.gq) + head * a.gq + j) * a.n_split + part;
+    const int64_t rec = many_record(a, part, token, head * a.gq + j);
     float* p = a.rec_o + rec * D + 4 * half;
 #pragma unroll
     for (int t = 0; t < 4; ++t)

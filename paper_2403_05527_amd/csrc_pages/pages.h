@@ -247,6 +247,22 @@ __device__ __forceinline__ int row_sees(const PageAttn& a, const SeqSpan& s, int
   return a.causal ? max(0, min(s.kv, s.kv - s.nq + row + 1)) : s.kv;
 }
 
+// What a block attends to, as the kernels ask for it: another kind of call has its own (these are gear_page_attn's).
+struct Span {
+  SeqSpan sp;
+  int begin;       // the first key of the block's parts, a multiple of MANY_KEYS
+  int table_row;
+};
+__device__ __forceinline__ Span span_of(const PageAttn& a, int s) { return Span{seq_span(a, s), 0, s}; }
+// whether the one part that a row has is its output, and where a part's record lies
+__device__ __forceinline__ bool is_output(const PageAttn&, const Span&, int parts) { return parts == 1; }
+__device__ __forceinline__ int64_t few_record(const PageAttn& a, int s, int head, int col, int part, int64_t, int) {
+  return (((int64_t)s * a.geom.H + head) * a.few_cols + col) * a.n_split + part;
+}
+__device__ __forceinline__ int64_t many_record(const PageAttn& a, int part, int64_t token, int query_head) {
+  return (token * ((int64_t)a.geom.H * a.gq) + query_head) * a.n_split + part;
+}
+
 // A sequence's row of the page table as a wave reads it: 64 entries at a time, one per lane, so that a step waits for the table once per 64
 // pages and not for each.
 struct PageRow {

@@ -1,0 +1,227 @@
+// Attention of a batch whose sequences share prefixes (include/gear.h).
+//
+// softmax over [prefix, own] is joined from parts: each part of the keys leaves its maximum, its sum of weights and its weighted sum of Values, and the parts are
+// brought to the greatest maximum.  The parts of a prefix take the columns of all the group's new tokens as one sequence's, with the keys that all of them see,
+// so a page is read once for 128 columns (32 in the kernel of few); what a sequence has behind the prefix is read as in gear_page_attn.  Both kinds of block run in one launch.
+// A prefix counts to the last whole 64 tokens that every new token of the group sees, so that no key of it is masked from anyone; what is left of it is read with
+// each sequence's own tokens.
+#include "page_few.h"
+#include "page_many.h"
+#include "page_merge.h"
+#include "shared.h"
+
+namespace gear {
+
+struct SharedPart : PageAttn {
+  const int32_t* group_start;
+  const int32_t* prefix_len;
+  int32_t n_groups, n_records, first_record;
+  bool prefix;
+};
+
+__device__ __forceinline__ int wave_least(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o));
+  return v;
+}
+__device__ __forceinline__ int group_bound(const SharedPart& a, int g) { return min(max(a.group_start[g], 0), a.n_seqs); }   // the first sequence of a group, the end of the one before
+// The prefix of a group as far as it counts: all lanes of the wave get it.
+__device__ __forceinline__ int shared_keys(const SharedPart& a, int g, int s0, int s1) {
+  int least = INT_MAX;
+  for (int base = s0; base < s1; base += 64) {
+    const int s = base + lane_id();
+    if (s >= s1) continue;
+    const SeqSpan sp = seq_span(a, s);
+    if (sp.nq > 0) least = min(least, a.causal ? sp.kv - sp.nq : sp.kv);
+  }
+  least = min(wave_least(least), a.prefix_len[g]);
+  return GEAR_WAVE_UNIFORM(max(least, 0) / MANY_KEYS * MANY_KEYS);
+}
+// The keys that sequence s shares.
+__device__ __forceinline__ int shared_before(const SharedPart& a, int s) {
+  int g = -1;
+  for (int base = 0; base < a.n_groups; base += 64) {
+    const int i = base + lane_id();
+    g += __popcll(__ballot(i < a.n_groups && group_bound(a, i) <= s));
+  }
+  if (g < 0) return 0;
+  const int s0 = group_bound(a, g), s1 = group_bound(a, g + 1);
+  return s < s1 ? shared_keys(a, g, s0, s1) : 0;
+}
+// A group's columns are those of its sequences, one behind the other.
+__device__ __forceinline__ SeqSpan group_rows(const SharedPart& a, int s0, int s1) {   // (kv: not set)
+  SeqSpan r{0, 0, 0};
+  if (s1 <= s0) return r;
+  r.q0 = max(a.q_start[s0], 0);
+  r.nq = min(max(a.q_start[s1], 0), a.n_tokens) - r.q0;
+  return r;
+}
+__device__ __forceinline__ Span span_of(const SharedPart& a, int s) {
+  if (!a.prefix) return Span{seq_span(a, s), shared_before(a, s), s};
+  const int s0 = group_bound(a, s), s1 = group_bound(a, s + 1);
+  Span r{group_rows(a, s0, s1), 0, s0};
+  if (r.sp.nq > 0) r.sp.kv = shared_keys(a, s, s0, s1);
+  if (r.sp.kv == 0) r.sp.nq = 0;
+  return r;
+}
+__device__ __forceinline__ bool is_output(const SharedPart& a, const Span& span, int parts) { return !a.prefix && span.begin == 0 && parts == 1; }
+__device__ __forceinline__ int64_t many_record(const SharedPart& a, int part, int64_t token, int query_head) {
+  return (token * ((int64_t)a.geom.H * a.gq) + query_head) * a.n_records + a.first_record + part;
+}
+__device__ __forceinline__ int64_t few_record(const SharedPart& a, int, int, int, int part, int64_t token, int query_head) { return many_record(a, part, token, query_head); }
+
+// Column tiles: of sequences as for gear_page_attn, of groups alike.
+__device__ __forceinline__ ColTile col_tile(const SharedPart& a, int i, int lane) {
+  if (!a.prefix) return col_tile(static_cast<const PageAttn&>(a), i, lane);
+  if (a.n_groups <= 64) {   // longest first
+    int kv = 0, tiles = 0, before = 0;
+    if (lane < a.n_groups) {
+      const SeqSpan sp = group_rows(a, group_bound(a, lane), group_bound(a, lane + 1));
+      kv = a.prefix_len[lane];
+      tiles = many_tiles(a, sp);
+    }
+    for (int j = 0; j < a.n_groups; ++j) {
+      const int kv_j = __builtin_amdgcn_readlane(kv, j), n = __builtin_amdgcn_readlane(tiles, j);
+      before += kv_j > kv || (kv_j == kv && j < lane) ? n : 0;
+    }
+    const unsigned long long mine = __ballot(i >= before && i < before + tiles);
+    if (mine == 0ull) return ColTile{-1, 0};
+    const int s = GEAR_WAVE_UNIFORM(__ffsll((long long)mine) - 1);
+    return ColTile{s, (__builtin_amdgcn_readlane(before + tiles, s) - 1 - i) * MANY_COLS};
+  }
+  // group g has the tiles from (its first row of q) * gq / 128 + g on
+  int g = -1;
+  for (int base = 0; base < a.n_groups; base += 64) {
+    const int j = base + lane;
+    g += __popcll(__ballot(j < a.n_groups && ((long long)max(a.q_start[group_bound(a, j < a.n_groups ? j : 0)], 0) * a.gq) / MANY_COLS + j <= i));
+  }
+  g = GEAR_WAVE_UNIFORM(g);
+  if (g < 0) return ColTile{-1, 0};
+  const SeqSpan sp = group_rows(a, group_bound(a, g), group_bound(a, g + 1));
+  const int local = i - (int)(((long long)sp.q0 * a.gq) / MANY_COLS + g);
+  return local >= 0 && local < many_tiles(a, sp) ? ColTile{g, local * MANY_COLS} : ColTile{-1, 0};
+}
+
+__device__ __forceinline__ SharedPart part_of(const SharedCall& c, const SharedKind& k, bool prefix) {
+  SharedPart p;
+  static_cast<PageAttn&>(p) = c.a;
+  p.group_start = c.group_start;
+  p.prefix_len = c.prefix_len;
+  p.n_groups = c.n_groups;
+  p.n_records = c.n_records;
+  p.first_record = prefix ? 0 : c.prefix.n_split;
+  p.prefix = prefix;
+  p.n_split = k.n_split;
+  p.least = k.least;
+  p.few = k.few;
+  p.tiles = k.tiles;
+  return p;
+}
+// (of a prefix: every row sees all of it, whatever the batch says of its new tokens.  `causal` is left for shared_keys.)
+__device__ __forceinline__ int row_sees(const SharedPart& a, const SeqSpan& s, int row) { return a.prefix ? s.kv : row_sees(static_cast<const PageAttn&>(a), s, row); }
+
+constexpr int SHARED_WAVES = MANY_THREADS / 64;
+
+// Blocks of many columns first (as in page_mixed.hip), the prefixes' before the others.
+template <int BITS, bool BF, int NC>
+__global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_shared_kernel(SharedCall c) {
+  GEAR_DYN_LDS(lds);
+  int bid = (int)blockIdx.x;
+  const int prefix_many = c.prefix.few > 0 ? 0 : c.prefix.blocks, many = prefix_many + c.own_many.blocks;
+  if (bid < many) {
+    const bool prefix = bid < prefix_many;
+    const SharedPart p = part_of(c, prefix ? c.prefix : c.own_many, prefix);
+    many_columns<BITS, BF, false>(p, prefix ? bid : bid - prefix_many, lds);
+  } else {
+    bid -= many;
+    const int prefix_few = c.prefix.blocks - prefix_many;
+    const bool prefix = bid < prefix_few;
+    const SharedPart p = part_of(c, prefix ? c.prefix : c.own_few, prefix);
+    few_columns<BITS, BF, NC, SHARED_WAVES>(p, prefix ? bid : bid - prefix_few, lds);
+  }
+}
+
+// The records of a row become its output: WAVES waves per token and query head.
+template <int WAVES>
+__global__ __launch_bounds__(256) void page_merge_shared_kernel(SharedCall c, int bf) {
+  GEAR_DYN_LDS(lds);
+  const SharedPart a = part_of(c, c.own_many, false);
+  const int lane = lane_id(), Hq = a.geom.H * a.gq, wave = (int)(threadIdx.x >> 6), mine = WAVES == 1 ? 0 : wave;
+  const int64_t id = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
+  const int token = (int)(id / Hq), jq = (int)(id - (int64_t)token * Hq), head = jq / a.gq;
+  if (token >= a.n_tokens) return;
+  int s = -1;
+  for (int base = 0; base < a.n_seqs; base += 64) {
+    const int i = base + lane;
+    s += __popcll(__ballot(i < a.n_seqs && a.q_start[i] <= token));
+  }
+  if (s < 0) return;
+  s = GEAR_WAVE_UNIFORM(s);
+  const Span span = span_of(a, s);
+  const SeqSpan& sp = span.sp;
+  const int row = token - sp.q0, cols = sp.nq * a.gq;
+  if (row < 0 || row >= sp.nq) return;
+  int own;
+  if (sp.nq <= c.own_few.few && cols <= c.own_few.few) {
+    own = parts_of(sp.kv - span.begin, c.own_few.n_split, c.own_few.least, KEY_STEP).count;
+  } else {
+    const int col = row * a.gq + (jq - head * a.gq), last = min(col / MANY_COLS * MANY_COLS + MANY_COLS, cols) - 1;
+    own = parts_of(row_sees(a, sp, last / a.gq) - span.begin, c.own_many.n_split, c.own_many.least, MANY_KEYS).count;
+  }
+  if (span.begin == 0 && own <= 1) return;
+  const int before = span.begin == 0 ? 0 : parts_of(span.begin, c.prefix.n_split, c.prefix.least, c.prefix.few > 0 ? KEY_STEP : MANY_KEYS).count;
+  const int count = before + own;
+  const int64_t rec = id * a.n_records, skip = c.prefix.n_split - before;   // (record i of the row: i, or i + skip behind the prefix's)
+  float top = -INFINITY;
+  for (int i = lane; i < count; i += 64) top = fmaxf(top, a.rec_ml[rec + i + (i < before ? 0 : skip)].x);
+  top = wave_max(top);
+  const float from = top == -INFINITY ? 0.0f : top;
+  Merged m{0.0f, 0.0f, 0.0f};
+  for (int i = mine; i < count; i += WAVES) {
+    const int64_t r = rec + i + (i < before ? 0 : skip);
+    const float2 ml = a.rec_ml[r], v = *reinterpret_cast<const float2*>(a.rec_o + r * D + 2 * lane);
+    const float by = GEAR_EXP2(ml.x - from);
+    m.sum += ml.y * by;
+    m.x += v.x * by;
+    m.y += v.y * by;
+  }
+  if constexpr (WAVES > 1) {
+    float* sums = reinterpret_cast<float*>(lds);
+    sums[(wave * 3 + 0) * 64 + lane] = m.sum;
+    sums[(wave * 3 + 1) * 64 + lane] = m.x;
+    sums[(wave * 3 + 2) * 64 + lane] = m.y;
+    block_lds_sync();
+    if (wave != 0) return;
+    for (int w = 1; w < WAVES; ++w) {
+      m.sum += sums[(w * 3 + 0) * 64 + lane];
+      m.x += sums[(w * 3 + 1) * 64 + lane];
+      m.y += sums[(w * 3 + 2) * 64 + lane];
+    }
+  }
+  store_merged(a, m, token, jq, lane, bf);
+}
+
+template <int BITS, bool BF, int NC>
+static hipError_t launch_shared(const SharedCall& c, hipStream_t st) {
+  const size_t need = few_lds_bytes<NC, SHARED_WAVES>(), lds = need > (size_t)MANY_LDS ? need : (size_t)MANY_LDS;   // 65 KB with two column tiles
+  static std::atomic<uint64_t> raised{0};
+  const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(page_attn_shared_kernel<BITS, BF, NC>), raised, lds, LDS_PER_CU);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((page_attn_shared_kernel<BITS, BF, NC>), dim3((unsigned)c.prefix.blocks + (unsigned)c.own_many.blocks + (unsigned)c.own_few.blocks), dim3(MANY_THREADS),
+                     lds, st, c);
+  return hipGetLastError();
+}
+
+hipError_t launch_page_shared(const SharedCall& c, int bits, bool bf, int tiles, hipStream_t st) {
+#define GEAR_SHARED(B) \
+  (tiles == 1 ? (bf ? launch_shared<B, true, 1>(c, st) : launch_shared<B, false, 1>(c, st)) : (bf ? launch_shared<B, true, 2>(c, st) : launch_shared<B, false, 2>(c, st)))
+  hipError_t e = bits == 16 ? GEAR_SHARED(16) : bits == 8 ? GEAR_SHARED(8) : GEAR_SHARED(4);
+#undef GEAR_SHARED
+  if (e != hipSuccess) return e;
+  const int64_t rows = (int64_t)c.a.n_tokens * c.a.geom.H * c.a.gq;
+  if (c.n_records <= 8) hipLaunchKernelGGL(page_merge_shared_kernel<1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, c, bf ? 1 : 0);
+  else hipLaunchKernelGGL(page_merge_shared_kernel<4>, dim3((unsigned)rows), dim3(256), (size_t)MERGE_LDS, st, c, bf ? 1 : 0);
+  return hipGetLastError();
+}
+
+}  // namespace gear
