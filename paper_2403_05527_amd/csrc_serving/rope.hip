@@ -4,6 +4,10 @@
 // once and used for all heads of the block.  The angle t w is reduced in 64 bits, in turns: t w / 2 pi less the nearest whole number, and of that the nearest quarter,
 // which leaves an angle of at most pi / 4 in fp32, for which the series of sine and cosine to the powers 9 and 10 are off by
 // (pi/4)^11 / 11! = 1.8e-9 and (pi/4)^12 / 12! = 1.2e-10, less than the roundings.
+//
+// Bound by the bytes: four prompts of 8192 tokens, 32 query heads and 8 KV heads, bf16, 805 MB in 144 us (5.6 TB/s; with one head per block, whose angles take
+// as long as its rows, 246); the Keys of 16 x 4096 tokens of 32 heads turned back, 1.07 GB in 183 (5.9 TB/s; 370).  Eight heads' rows requested at once against
+// four: 200 -> 183 us there, 151 -> 145 in the first; 16 heads per block 149 in the first, 4 in an 8-bit pool 199 instead of 182.
 #include "page_piece.h"
 #include "serving.h"
 
@@ -103,8 +107,19 @@ __device__ __forceinline__ uint4 turned(const Rope& r, const LaneTurns& t, const
   return make_uint4(turn_pair<BF>(v.x, o.x, t, 0), turn_pair<BF>(v.y, o.y, t, 2), turn_pair<BF>(v.z, o.z, t, 4), turn_pair<BF>(v.w, o.w, t, 6));
 }
 
-// grid: (part of the heads, 16 tokens of one sequence).  BITS: of the pool's rows, 0 where there is none.
-template <int BITS, bool BF, int PAIRS>
+// (rows that are read once need no place in the caches: 2 us of 184 where 8-bit pages are written)
+__device__ __forceinline__ uint4 load16_once(const unsigned char* p) {
+#ifdef GEAR_NO_NONTEMPORAL
+  return *reinterpret_cast<const uint4*>(p);
+#else
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p)));
+#endif
+}
+
+// grid: (part of the heads, 16 tokens of one sequence).  BITS: of the pool's rows, 0 where there is none.  A block has up to HEADS heads at a time on their way.
+// PAST: `out` is large (PAST_CACHES).  (As a branch at the store it was lost: both stores became one.)
+constexpr int HEADS = 8;
+template <int BITS, bool BF, int PAIRS, bool PAST>
 __global__ __launch_bounds__(ROPE_THREADS) void rope_kernel(RopeRows a) {
   const unsigned bid = blockIdx.x, rest = bid / (unsigned)a.parts, s = rest / (unsigned)a.chunks;
   const int part = (int)(bid - rest * (unsigned)a.parts), c = threadIdx.x & 15, in_chunk = threadIdx.x >> 4;
@@ -113,37 +128,54 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_kernel(RopeRows a) {
   const int64_t at = (int64_t)s * a.n_rows + (there ? row : a.n_rows - 1);
   const int64_t position = a.positions[at];
   if (BITS == 0 || part < a.x_parts) {
-    const LaneTurns t = lane_turns<PAIRS>(a.rope, c, position);
     const unsigned char* xp = a.x.data + 2 * ((int64_t)s * a.x.seq + (int64_t)(there ? row : 0) * a.x.token);
     unsigned char* op = a.out.data + 2 * ((int64_t)s * a.out.seq + (int64_t)(there ? row : 0) * a.out.token);
     const int h0 = part * a.per, h1 = min(a.heads, h0 + a.per);
-    for (int h = h0; h < h1; ++h) {
-      const unsigned char* from = xp + 2 * (h * a.x.head);
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (there) v = *reinterpret_cast<const uint4*>(from + 16 * c);
-      v = turned<BF, PAIRS>(a.rope, t, v, from, c, there);
-      if (there) *reinterpret_cast<uint4*>(op + 2 * (h * a.out.head) + 16 * c) = v;
+    LaneTurns t;
+    for (int h = h0; h < h1; h += HEADS) {
+      uint4 v[HEADS];
+#pragma unroll
+      for (int u = 0; u < HEADS; ++u) {
+        v[u] = make_uint4(0, 0, 0, 0);
+        if (there && h + u < h1) v[u] = load16_once(xp + 2 * ((h + u) * a.x.head) + 16 * c);
+      }
+      if (h == h0) t = lane_turns<PAIRS>(a.rope, c, position);   // (behind the first requests)
+#pragma unroll
+      for (int u = 0; u < HEADS; ++u) {
+        if (h + u >= h1) continue;
+        const uint4 y = turned<BF, PAIRS>(a.rope, t, v[u], xp + 2 * ((h + u) * a.x.head), c, there);
+        unsigned char* to = op + 2 * ((h + u) * a.out.head) + 16 * c;
+        if (there) store16<PAST>(to, y);
+      }
     }
   } else if constexpr (BITS != 0) {
     const PageGeom& g = a.geom;
     const int64_t slot = there ? a.slots[at] : -1;
     const bool live = slot >= 0 && slot < (int64_t)g.n_pages << g.shift;   // the same for the 16 lanes of a row
-    const LaneTurns t = lane_turns<PAIRS>(a.rope, c, position);
     const int64_t to = live ? slot : 0;
     const int in_page = (int)(to & page_mask(g));
-    const int64_t k_row = (int64_t)s * a.k.seq + (int64_t)(there ? row : 0) * a.k.token, v_row = (int64_t)s * a.v.seq + (int64_t)(there ? row : 0) * a.v.token;
+    const unsigned char* kp = a.k.data + 2 * ((int64_t)s * a.k.seq + (int64_t)(there ? row : 0) * a.k.token);
+    const unsigned char* vp = a.v.data + 2 * ((int64_t)s * a.v.seq + (int64_t)(there ? row : 0) * a.v.token);
     const int h0 = (part - a.x_parts) * a.kv_per, h1 = min(g.H, h0 + a.kv_per);
-    for (int h = h0; h < h1; ++h) {
-      const unsigned char* kp = a.k.data + 2 * (k_row + h * a.k.head);
-      const unsigned char* vp = a.v.data + 2 * (v_row + h * a.v.head);
-      uint4 k = make_uint4(0, 0, 0, 0), v = k;
-      if (there) {
-        k = *reinterpret_cast<const uint4*>(kp + 16 * c);
-        v = *reinterpret_cast<const uint4*>(vp + 16 * c);
+    LaneTurns t;
+    for (int h = h0; h < h1; h += HEADS / 2) {
+      uint4 k[HEADS / 2], v[HEADS / 2];
+#pragma unroll
+      for (int u = 0; u < HEADS / 2; ++u) {
+        k[u] = v[u] = make_uint4(0, 0, 0, 0);
+        if (there && h + u < h1) {
+          k[u] = *reinterpret_cast<const uint4*>(kp + 2 * ((h + u) * a.k.head) + 16 * c);
+          v[u] = *reinterpret_cast<const uint4*>(vp + 2 * ((h + u) * a.v.head) + 16 * c);
+        }
       }
-      unsigned char* block = const_cast<unsigned char*>(block_of(g, (int)(to >> g.shift), h, 0));
-      store_piece<BITS, BF>(g, block, in_page, c, turned<BF, PAIRS>(a.rope, t, k, kp, c, there), live);
-      store_piece<BITS, BF>(g, block + g.block_bytes, in_page, c, v, live);
+      if (h == h0) t = lane_turns<PAIRS>(a.rope, c, position);
+#pragma unroll
+      for (int u = 0; u < HEADS / 2; ++u) {
+        if (h + u >= h1) continue;
+        unsigned char* block = const_cast<unsigned char*>(block_of(g, (int)(to >> g.shift), h + u, 0));
+        store_piece<BITS, BF>(g, block, in_page, c, turned<BF, PAIRS>(a.rope, t, k[u], kp + 2 * ((h + u) * a.k.head), c, there), live);
+        store_piece<BITS, BF>(g, block + g.block_bytes, in_page, c, v[u], live);
+      }
     }
   }
 }
@@ -151,7 +183,8 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_kernel(RopeRows a) {
 template <int BITS, bool BF, int PAIRS>
 static hipError_t launch(const RopeRows& a, int n_seqs, hipStream_t st) {
   const int64_t blocks = (int64_t)n_seqs * a.chunks * a.parts;
-  hipLaunchKernelGGL((rope_kernel<BITS, BF, PAIRS>), dim3((unsigned)blocks), dim3(ROPE_THREADS), 0, st, a);
+  if ((int64_t)n_seqs * a.n_rows * a.heads * 2 * D >= PAST_CACHES) hipLaunchKernelGGL((rope_kernel<BITS, BF, PAIRS, true>), dim3((unsigned)blocks), dim3(ROPE_THREADS), 0, st, a);
+  else hipLaunchKernelGGL((rope_kernel<BITS, BF, PAIRS, false>), dim3((unsigned)blocks), dim3(ROPE_THREADS), 0, st, a);
   return hipGetLastError();
 }
 template <int BITS, bool BF>
@@ -162,6 +195,7 @@ static hipError_t launch(const RopeRows& a, bool interleaved, int n_seqs, hipStr
   return launch<BITS, BF, PAIRS_ANY>(a, n_seqs, st);
 }
 
+constexpr int ROPE_HEADS_MOST = HEADS;   // of a block
 static bool one_run(const RowView& r, int64_t n_rows) { return !r.data || r.seq == n_rows * r.token; }
 
 hipError_t launch_rope(const RopeRows& call, int bits, bool bf, bool interleaved, int n_seqs, hipStream_t st) {
@@ -175,8 +209,11 @@ hipError_t launch_rope(const RopeRows& call, int bits, bool bf, bool interleaved
     n_seqs = 1;
   }
   a.chunks = (a.n_rows + ROPE_TOKENS - 1) / ROPE_TOKENS;
-  a.per = a.kv_per = 1;
   const int H = bits ? a.geom.H : 0;
+  // Heads of a block: one where there are few blocks, as many as leave 8 blocks per CU
+  const int64_t rows = (int64_t)n_seqs * a.chunks, per = rows * (a.heads + 2 * H) / (8 * GEAR_CUS);
+  a.per = per < 1 ? 1 : per < ROPE_HEADS_MOST ? (int)per : ROPE_HEADS_MOST;
+  a.kv_per = (a.per + 1) / 2;
   a.x_parts = (a.heads + a.per - 1) / a.per;
   a.parts = a.x_parts + (H + a.kv_per - 1) / a.kv_per;
   switch (bits) {
