@@ -20,24 +20,60 @@ struct SharedPart : PageAttn {
 };
 
 __device__ __forceinline__ int wave_least(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o));
-  return v;
+  v = min(v, (int)dpp_u<DPP_XOR1>((uint32_t)v));
+  v = min(v, (int)dpp_u<DPP_XOR2>((uint32_t)v));
+  v = min(v, (int)dpp_u<DPP_HALF_MIRROR>((uint32_t)v));
+  v = min(v, (int)dpp_u<DPP_MIRROR>((uint32_t)v));
+  uint32_t x = (uint32_t)v, y = x;
+  GEAR_LANE_SWAP16(x, y);
+  v = min((int)x, (int)y);
+  x = y = (uint32_t)v;
+  GEAR_LANE_SWAP32(x, y);
+  return min((int)x, (int)y);
 }
 __device__ __forceinline__ int group_bound(const SharedPart& a, int g) { return min(max(a.group_start[g], 0), a.n_seqs); }   // the first sequence of a group, the end of the one before
-// The prefix of a group as far as it counts: all lanes of the wave get it.
-__device__ __forceinline__ int shared_keys(const SharedPart& a, int g, int s0, int s1) {
+// The keys that a row count and a length leave before the first new token, which all new tokens see (no new tokens: any number).
+__device__ __forceinline__ int keys_before(const SharedPart& a, const SeqSpan& sp) { return sp.nq <= 0 ? INT_MAX : a.causal ? sp.kv - sp.nq : sp.kv; }
+__device__ __forceinline__ int whole_tiles(int keys) { return GEAR_WAVE_UNIFORM(max(keys, 0) / MANY_KEYS * MANY_KEYS); }
+
+// A call of up to 64 sequences and 63 groups as a wave has it: sequence i and group i in lane i, so that whatever a block has to know of them is one trip to memory
+// (one after the other, which group, its sequences, their lengths, it took 4 us of the 15 of a small call).
+struct Lanes {
+  SeqSpan sp;    // of sequence i
+  int start;     // the first sequence of group i
+  int len;       // prefix_len[i]
+};
+__device__ __forceinline__ bool fits_lanes(const SharedPart& a) { return a.n_seqs <= 64 && a.n_groups < 64; }
+__device__ __forceinline__ Lanes load_lanes(const SharedPart& a, int lane) {
+  Lanes l;
+  l.sp = seq_span(a, min(lane, a.n_seqs - 1));
+  l.start = group_bound(a, min(lane, a.n_groups));
+  l.len = a.prefix_len[min(lane, a.n_groups - 1)];
+  return l;
+}
+__device__ __forceinline__ SeqSpan lane_span(const Lanes& l, int s) {
+  return SeqSpan{__builtin_amdgcn_readlane(l.sp.q0, s), __builtin_amdgcn_readlane(l.sp.nq, s), __builtin_amdgcn_readlane(l.sp.kv, s)};
+}
+__device__ __forceinline__ int lane_keys(const SharedPart& a, const Lanes& l, int lane, int g, int s0, int s1) {
+  const int least = wave_least(lane >= s0 && lane < s1 ? keys_before(a, l.sp) : INT_MAX);
+  return whole_tiles(min(least, __builtin_amdgcn_readlane(l.len, g)));
+}
+__device__ __forceinline__ int lane_before(const SharedPart& a, const Lanes& l, int lane, int s) {   // the keys that sequence s shares
+  const int g = __popcll(__ballot(lane < a.n_groups && l.start <= s)) - 1;
+  if (g < 0) return 0;
+  const int s0 = __builtin_amdgcn_readlane(l.start, g), s1 = __builtin_amdgcn_readlane(l.start, g + 1);
+  return s < s1 ? lane_keys(a, l, lane, g, s0, s1) : 0;
+}
+
+// The same from memory, for any number of them.
+__device__ __forceinline__ int shared_keys(const SharedPart& a, int g, int s0, int s1) {   // the prefix of group g, as far as it counts
   int least = INT_MAX;
   for (int base = s0; base < s1; base += 64) {
     const int s = base + lane_id();
-    if (s >= s1) continue;
-    const SeqSpan sp = seq_span(a, s);
-    if (sp.nq > 0) least = min(least, a.causal ? sp.kv - sp.nq : sp.kv);
+    if (s < s1) least = min(least, keys_before(a, seq_span(a, s)));
   }
-  least = min(wave_least(least), a.prefix_len[g]);
-  return GEAR_WAVE_UNIFORM(max(least, 0) / MANY_KEYS * MANY_KEYS);
+  return whole_tiles(min(wave_least(least), a.prefix_len[g]));
 }
-// The keys that sequence s shares.
 __device__ __forceinline__ int shared_before(const SharedPart& a, int s) {
   int g = -1;
   for (int base = 0; base < a.n_groups; base += 64) {
@@ -57,10 +93,23 @@ __device__ __forceinline__ SeqSpan group_rows(const SharedPart& a, int s0, int s
   return r;
 }
 __device__ __forceinline__ Span span_of(const SharedPart& a, int s) {
-  if (!a.prefix) return Span{seq_span(a, s), shared_before(a, s), s};
-  const int s0 = group_bound(a, s), s1 = group_bound(a, s + 1);
-  Span r{group_rows(a, s0, s1), 0, s0};
-  if (r.sp.nq > 0) r.sp.kv = shared_keys(a, s, s0, s1);
+  Span r;
+  if (fits_lanes(a)) {
+    const int lane = lane_id();
+    const Lanes l = load_lanes(a, lane);
+    if (!a.prefix) return Span{lane_span(l, s), lane_before(a, l, lane, s), s};
+    const int s0 = __builtin_amdgcn_readlane(l.start, s), s1 = __builtin_amdgcn_readlane(l.start, s + 1);
+    r = Span{SeqSpan{0, 0, 0}, 0, s0};
+    if (s1 > s0) {
+      const SeqSpan first = lane_span(l, s0), last = lane_span(l, s1 - 1);
+      r.sp = SeqSpan{first.q0, last.q0 + last.nq - first.q0, lane_keys(a, l, lane, s, s0, s1)};
+    }
+  } else {
+    if (!a.prefix) return Span{seq_span(a, s), shared_before(a, s), s};
+    const int s0 = group_bound(a, s), s1 = group_bound(a, s + 1);
+    r = Span{group_rows(a, s0, s1), 0, s0};
+    if (r.sp.nq > 0) r.sp.kv = shared_keys(a, s, s0, s1);
+  }
   if (r.sp.kv == 0) r.sp.nq = 0;
   return r;
 }
@@ -75,10 +124,15 @@ __device__ __forceinline__ ColTile col_tile(const SharedPart& a, int i, int lane
   if (!a.prefix) return col_tile(static_cast<const PageAttn&>(a), i, lane);
   if (a.n_groups <= 64) {   // longest first
     int kv = 0, tiles = 0, before = 0;
-    if (lane < a.n_groups) {
-      const SeqSpan sp = group_rows(a, group_bound(a, lane), group_bound(a, lane + 1));
+    if (fits_lanes(a)) {
+      const Lanes l = load_lanes(a, lane);
+      const int end = __shfl(l.start, min(lane + 1, 63));   // (lanes from n_groups on have the last group's end)
+      const int q0 = __shfl(l.sp.q0, min(l.start, 63)), q1 = __shfl(l.sp.q0 + l.sp.nq, max(end - 1, 0));
+      kv = l.len;
+      tiles = lane < a.n_groups && end > l.start ? many_tiles(a, SeqSpan{q0, q1 - q0, 0}) : 0;
+    } else if (lane < a.n_groups) {
       kv = a.prefix_len[lane];
-      tiles = many_tiles(a, sp);
+      tiles = many_tiles(a, group_rows(a, group_bound(a, lane), group_bound(a, lane + 1)));
     }
     for (int j = 0; j < a.n_groups; ++j) {
       const int kv_j = __builtin_amdgcn_readlane(kv, j), n = __builtin_amdgcn_readlane(tiles, j);
@@ -141,7 +195,17 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void page_attn_shared_kernel(Share
   }
 }
 
-// The records of a row become its output: WAVES waves per token and query head.
+// Where no block has many columns: without the registers that those need, four blocks to a CU.
+template <int BITS, bool BF, int NC>
+__global__ __launch_bounds__(64 * SHARED_WAVES) void page_attn_shared_few_kernel(SharedCall c) {
+  GEAR_DYN_LDS(lds);
+  const int bid = (int)blockIdx.x;
+  const bool prefix = bid < c.prefix.blocks;
+  const SharedPart p = part_of(c, prefix ? c.prefix : c.own_few, prefix);
+  few_columns<BITS, BF, NC, SHARED_WAVES>(p, prefix ? bid : bid - c.prefix.blocks, lds);
+}
+
+// The records of a row become its output: WAVES waves per token and query head, eight records of each on their way, the first of them requested with the lengths.
 template <int WAVES>
 __global__ __launch_bounds__(256) void page_merge_shared_kernel(SharedCall c, int bf) {
   GEAR_DYN_LDS(lds);
@@ -150,10 +214,22 @@ __global__ __launch_bounds__(256) void page_merge_shared_kernel(SharedCall c, in
   const int64_t id = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
   const int token = (int)(id / Hq), jq = (int)(id - (int64_t)token * Hq), head = jq / a.gq;
   if (token >= a.n_tokens) return;
+  const int64_t rec = id * a.n_records;
+  float2 ml[8], v[8];
+  auto request = [&](int i0) {   // in the row, whether they have been written or not
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int64_t r = rec + min(i0 + WAVES * u, a.n_records - 1);
+      ml[u] = a.rec_ml[r];
+      v[u] = *reinterpret_cast<const float2*>(a.rec_o + r * D + 2 * lane);
+    }
+  };
+  request(mine);
+  float top = a.rec_ml[rec + min(lane, a.n_records - 1)].x;
   int s = -1;
   for (int base = 0; base < a.n_seqs; base += 64) {
     const int i = base + lane;
-    s += __popcll(__ballot(i < a.n_seqs && a.q_start[i] <= token));
+    s += __popcll(__ballot(i < a.n_seqs && a.q_start[min(i, a.n_seqs - 1)] <= token));
   }
   if (s < 0) return;
   s = GEAR_WAVE_UNIFORM(s);
@@ -170,20 +246,24 @@ __global__ __launch_bounds__(256) void page_merge_shared_kernel(SharedCall c, in
   }
   if (span.begin == 0 && own <= 1) return;
   const int before = span.begin == 0 ? 0 : parts_of(span.begin, c.prefix.n_split, c.prefix.least, c.prefix.few > 0 ? KEY_STEP : MANY_KEYS).count;
-  const int count = before + own;
-  const int64_t rec = id * a.n_records, skip = c.prefix.n_split - before;   // (record i of the row: i, or i + skip behind the prefix's)
-  float top = -INFINITY;
-  for (int i = lane; i < count; i += 64) top = fmaxf(top, a.rec_ml[rec + i + (i < before ? 0 : skip)].x);
+  const int first_own = c.prefix.n_split;
+  auto written = [&](int i) { return i < before || (i >= first_own && i < first_own + own); };
+  top = written(lane) ? top : -INFINITY;
+  for (int i = lane + 64; i < a.n_records; i += 64)
+    if (written(i)) top = fmaxf(top, a.rec_ml[rec + i].x);
   top = wave_max(top);
   const float from = top == -INFINITY ? 0.0f : top;
   Merged m{0.0f, 0.0f, 0.0f};
-  for (int i = mine; i < count; i += WAVES) {
-    const int64_t r = rec + i + (i < before ? 0 : skip);
-    const float2 ml = a.rec_ml[r], v = *reinterpret_cast<const float2*>(a.rec_o + r * D + 2 * lane);
-    const float by = GEAR_EXP2(ml.x - from);
-    m.sum += ml.y * by;
-    m.x += v.x * by;
-    m.y += v.y * by;
+  for (int i0 = mine; i0 < a.n_records; i0 += WAVES * 8) {
+    if (i0 != mine) request(i0);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const bool there = written(i0 + WAVES * u);
+      const float by = there ? GEAR_EXP2(ml[u].x - from) : 0.0f;
+      m.sum += there ? ml[u].y * by : 0.0f;
+      m.x += there ? v[u].x * by : 0.0f;
+      m.y += there ? v[u].y * by : 0.0f;
+    }
   }
   if constexpr (WAVES > 1) {
     float* sums = reinterpret_cast<float*>(lds);
@@ -203,6 +283,14 @@ __global__ __launch_bounds__(256) void page_merge_shared_kernel(SharedCall c, in
 
 template <int BITS, bool BF, int NC>
 static hipError_t launch_shared(const SharedCall& c, hipStream_t st) {
+  if (c.own_many.blocks == 0 && c.prefix.few > 0) {
+    constexpr size_t few = few_lds_bytes<NC, SHARED_WAVES>();   // 33 KB for each column tile
+    static std::atomic<uint64_t> raised_few{0};
+    const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(page_attn_shared_few_kernel<BITS, BF, NC>), raised_few, few, LDS_PER_CU);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((page_attn_shared_few_kernel<BITS, BF, NC>), dim3((unsigned)c.prefix.blocks + (unsigned)c.own_few.blocks), dim3(64 * SHARED_WAVES), few, st, c);
+    return hipGetLastError();
+  }
   const size_t need = few_lds_bytes<NC, SHARED_WAVES>(), lds = need > (size_t)MANY_LDS ? need : (size_t)MANY_LDS;   // 65 KB with two column tiles
   static std::atomic<uint64_t> raised{0};
   const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(page_attn_shared_kernel<BITS, BF, NC>), raised, lds, LDS_PER_CU);
