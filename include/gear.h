@@ -437,6 +437,8 @@ typedef struct gear_page_groups {
   int32_t n_groups;
   int32_t max_q;                /* no group has more rows of q (the rows of one that has may stay)     */
   int32_t max_prefix;           /* about the longest prefix: what the work is divided by               */
+  int32_t always;               /* 0: prefixes are shared where that is estimated to be faster, else the call is gear_page_attn's; */
+                                /* 1: always (but where a workspace of 512 MB would not do)            */
   const int32_t* group_start;   /* device [n_groups + 1], ascending: group i has sequences group_start[i] .. */
   const int32_t* prefix_len;    /* device [n_groups]: the first tokens that are the same in all of them; they are read through the
                                  * group's first sequence's row of the page table.  Where the sequences part within a page, each may have its own copy. */

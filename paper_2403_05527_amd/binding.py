@@ -65,7 +65,7 @@ class gear_page_table(ctypes.Structure):
 
 
 class gear_page_groups(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int32) for n in ("n_groups", "max_q", "max_prefix")] + [(n, ctypes.c_void_p) for n in ("group_start", "prefix_len")]
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_groups", "max_q", "max_prefix", "always")] + [(n, ctypes.c_void_p) for n in ("group_start", "prefix_len")]
 
 
 GEAR_PAGE_LIST_MAX = 1024
@@ -484,11 +484,11 @@ def gear_page_move(cfg, pool, pairs):
 
 
 # ---- attention with shared prefixes
-def make_page_groups(group_start, prefix_len, max_q, max_prefix):
+def make_page_groups(group_start, prefix_len, max_q, max_prefix, always=False):
     """The groups of a batch: int32 tensors group_start [n_groups + 1], prefix_len [n_groups], which it keeps alive."""
     n = prefix_len.numel()
     d = _page_device()
-    g = gear_page_groups(n, max_q, max_prefix, _page_index(group_start, torch.int32, n + 1, d, "group_start"),
+    g = gear_page_groups(n, max_q, max_prefix, 1 if always else 0, _page_index(group_start, torch.int32, n + 1, d, "group_start"),
                          _page_index(prefix_len, torch.int32, n, d, "prefix_len"))
     g.tensors, g.device = (group_start, prefix_len), d
     return g

@@ -84,6 +84,24 @@ __device__ __forceinline__ int shared_before(const SharedPart& a, int s) {
   const int s0 = group_bound(a, g), s1 = group_bound(a, g + 1);
   return s < s1 ? shared_keys(a, g, s0, s1) : 0;
 }
+// What lies behind the prefixes, longest first: those that begin when the prefixes' blocks have ended are short.
+__device__ __forceinline__ int few_sequence(const SharedPart& a, int i) {
+  if (a.prefix || !fits_lanes(a)) return i;
+  const int lane = lane_id();
+  const Lanes l = load_lanes(a, lane);
+  int own = lane < a.n_seqs ? l.sp.kv : -1;
+  for (int g = 0; g < a.n_groups; ++g) {
+    const int s0 = __builtin_amdgcn_readlane(l.start, g), s1 = __builtin_amdgcn_readlane(l.start, g + 1), len = max(__builtin_amdgcn_readlane(l.len, g), 0);
+    if (lane >= s0 && lane < s1) own = max(own - len, 0);
+  }
+  int before = 0;
+  for (int j = 0; j < a.n_seqs; ++j) {
+    const int other = __builtin_amdgcn_readlane(own, j);
+    before += other > own || (other == own && j < lane) ? 1 : 0;
+  }
+  return GEAR_WAVE_UNIFORM(__ffsll((long long)__ballot(lane < a.n_seqs && before == i)) - 1);
+}
+
 // A group's columns are those of its sequences, one behind the other.
 __device__ __forceinline__ SeqSpan group_rows(const SharedPart& a, int s0, int s1) {   // (kv: not set)
   SeqSpan r{0, 0, 0};
@@ -307,7 +325,7 @@ hipError_t launch_page_shared(const SharedCall& c, int bits, bool bf, int tiles,
 #undef GEAR_SHARED
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)c.a.n_tokens * c.a.geom.H * c.a.gq;
-  if (c.n_records <= 8) hipLaunchKernelGGL(page_merge_shared_kernel<1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, c, bf ? 1 : 0);
+  if (c.n_records <= 32) hipLaunchKernelGGL(page_merge_shared_kernel<1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, c, bf ? 1 : 0);
   else hipLaunchKernelGGL(page_merge_shared_kernel<4>, dim3((unsigned)rows), dim3(256), (size_t)MERGE_LDS, st, c, bf ? 1 : 0);
   return hipGetLastError();
 }

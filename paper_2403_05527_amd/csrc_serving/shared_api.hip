@@ -14,38 +14,73 @@ static int64_t records_bound(int64_t rows, int max_kv, int max_prefix) {
   return std::min(RECORDS_MOST, std::min(by_blocks, by_keys));
 }
 
+// Estimates of a call's time, in ns; they choose the parts of the prefixes, and whether they are shared at all.
+struct Parted {
+  int n;
+  double time;
+};
+// The number of equal parts of the prefixes that is the fastest: `blocks` of them undivided, of which `filled` have keys; a part takes 8 us and, per `step` keys, `alone`, or
+// `beside` where two blocks share a CU.  What lies behind takes `own` by itself, and runs on the places that the prefixes' blocks leave until they have ended; the records (`records` bytes per
+// part) are written and read at 5 TB/s.  Where much lies behind, the prefixes' blocks are no more than the CUs.
+// 64 sequences behind 8192 tokens, bf16, 8 KV heads, 100 to 1000 tokens of their own (37 us by themselves): 76, 50, 47, 54, 52 and 62 us in 4, 8, 12, 16, 24 and 32 parts, and 6 to 12
+// of joining; five groups of 1500 to 6001 tokens at 8 bits 47, 32, 34, 37 and 40 in 4, 8, 10, 12 and 24.  Prefixes alone, in 4, 8, 16 and 32 parts: 1024 tokens 13, 11, 11 and 14 us,
+// 16384 111, 62, 38 and 31.
+static Parted prefix_parts(double blocks, double filled, int most, int keys, int step, double alone, double beside, double own, double records) {
+  Parted best{1, 0.0};
+  for (int n = 1; n <= most; ++n) {
+    const double real = blocks * filled * n, steps = (double)((((int64_t)keys + n - 1) / n + step - 1) / step);
+    if (n > 1 && own > 10000.0 && real > GEAR_PAGE_CUS) break;
+    const double left = real < MANY_SLOTS ? 1.0 - real / MANY_SLOTS : 0.0;   // of the places
+    double block = steps * beside;
+    if (real <= GEAR_PAGE_CUS && block > own / left) block = own / left + (steps - own / left / beside) * alone;
+    const double prefix = std::ceil(real / MANY_SLOTS) * (8000.0 + block), rest = own - prefix * left, t = prefix + (rest > 0.0 ? rest : 0.0) + records * n * 2.0 / 5000.0;
+    if (n == 1 || t < best.time) best = Parted{n, t};
+  }
+  return best;
+}
+
 static SharedPlan shared_plan(int H, int gq, const gear_page_batch& b, const gear_page_groups& gr, int bytes_per_key) {
   SharedPlan p{};
-  const int64_t rows = (int64_t)b.n_tokens * H * gq;
-  // Sequences that have a tile of 128 columns to themselves read a page no more often by themselves than as a group, and need no records for it.
-  p.shared = gr.n_groups > 0 && gr.max_prefix >= MANY_KEYS && (int64_t)b.n_tokens * gq < (int64_t)MANY_COLS * b.n_seqs && 2 * rows <= RECORDS_MOST;
-  if (!p.shared) return p;
-  const int64_t seq_cols = (int64_t)b.max_q * gq, group_cols = std::min((int64_t)gr.max_q, (int64_t)b.n_tokens) * gq, all_cols = (int64_t)b.n_tokens * gq;
+  const int64_t rows = (int64_t)b.n_tokens * H * gq, all_cols = (int64_t)b.n_tokens * gq;
+  if (gr.n_groups == 0 || gr.max_prefix < MANY_KEYS || 2 * rows > RECORDS_MOST) return p;
+  const int64_t seq_cols = (int64_t)b.max_q * gq, group_cols = std::min((int64_t)gr.max_q, (int64_t)b.n_tokens) * gq;
   const bool prefix_few = group_cols <= FEW_COLS_MOST;
-  const int prefix = std::min(gr.max_prefix, b.max_kv), own = std::max(b.max_kv - prefix, 1);
+  const int prefix = std::min(gr.max_prefix, std::max(b.max_kv, MANY_KEYS)), own = std::max(b.max_kv - prefix, 1);
   const bool uniform = (int64_t)b.n_seqs * b.max_q == b.n_tokens, all_few = seq_cols <= FEW_COLS_MOST;
   const bool few = all_few || (!uniform && gq <= FEW_COLS_MOST), many = !all_few;
   const int few_limit = !few ? 0 : all_few ? (int)seq_cols : gq <= 16 ? 16 : FEW_COLS_MOST;
   p.tiles = few_limit <= 16 && (!prefix_few || group_cols <= 16) ? 1 : 2;
-  // parts of the prefixes
-  const int64_t tiles = prefix_few ? gr.n_groups : std::max((all_cols + MANY_COLS - 1) / MANY_COLS, (int64_t)gr.n_groups);
-  p.prefix.few = prefix_few ? (int)group_cols : 0;
-  p.prefix.tiles = (int)(all_cols / MANY_COLS + gr.n_groups);
-  const double bytes = (double)gr.n_groups * H * prefix * bytes_per_key / 6e3;   // ns
-  p.prefix.n_split = best_parts(tiles * H, 1.0, MANY_SLOTS, MANY_BLOCKS_MOST, prefix, prefix_few ? FEW_PART : MANY_PART, 6000.0, prefix_few ? FEW_PART / 2 : MANY_KEYS, 1.0, bytes,
-                                (double)rows * RECORD_BYTES, 0.0);
-  while (p.prefix.n_split > 1 && rows * p.prefix.n_split > DIVIDED_MOST) --p.prefix.n_split;
-  p.prefix.least = std::max(prefix / p.prefix.n_split, prefix_few ? FEW_PART : MANY_PART);
-  // ... and of what lies behind
+  const double record_bytes = (double)rows * RECORD_BYTES, codes = bytes_per_key < 4 * D ? 1.3 : 1.0;
+  // parts of what lies behind the prefixes
   p.own_few = SharedKind{1, FEW_PART, few_limit, 0, 0};
   p.own_many = SharedKind{1, MANY_PART, few_limit, (int)(all_cols / MANY_COLS + b.n_seqs), 0};
   if (few) {
-    p.own_few.n_split = best_parts((int64_t)b.n_seqs * H, 1.0, FEW_SLOTS, FEW_BLOCKS_MOST, own, FEW_PART, 4000.0, FEW_PART / 2, 1.0, 0.0, (double)rows * RECORD_BYTES, 0.0);
+    p.own_few.n_split = best_parts((int64_t)b.n_seqs * H, 1.0, FEW_SLOTS, FEW_BLOCKS_MOST, own, FEW_PART, 4000.0, FEW_PART / 2, 1.0, 0.0, record_bytes, 0.0);
     while (p.own_few.n_split > 1 && rows * p.own_few.n_split > DIVIDED_MOST) --p.own_few.n_split;
   }
+  // ... and of the prefixes, for each tile of columns
+  const int64_t tiles = prefix_few ? gr.n_groups : std::max((all_cols + MANY_COLS - 1) / MANY_COLS, (int64_t)gr.n_groups);
+  p.prefix.few = prefix_few ? (int)group_cols : 0;
+  p.prefix.tiles = (int)(all_cols / MANY_COLS + gr.n_groups);
+  const int least = prefix_few ? FEW_PART : MANY_PART;
+  const int64_t by_blocks = MANY_BLOCKS_MOST / std::max(tiles * H, (int64_t)1), by_records = std::max(DIVIDED_MOST / rows, (int64_t)1);
+  const int most = (int)std::max((int64_t)1, std::min((int64_t)(prefix / least), std::min(by_blocks, by_records)));
+  const double filled = gr.n_groups >= 4 ? 0.65 : 1.0, own_ns = 6000.0 + 0.6 * (double)b.n_seqs * H * own * bytes_per_key / 4.5e3;
+  const Parted parts = prefix_few ? prefix_parts((double)(tiles * H), filled, most, prefix, FEW_PART / 2, 2000.0, 2500.0, own_ns, record_bytes)
+                                  : prefix_parts((double)(tiles * H), filled, most, prefix, MANY_KEYS, 1500.0 * codes, 2360.0 * codes, own_ns, record_bytes);
+  p.prefix.n_split = parts.n;
+  p.prefix.least = std::max(prefix / parts.n, least);
   p.own_few.blocks = few ? 1 : 0;
   p.own_many.blocks = many ? 1 : 0;
-  p.records = rows * (p.prefix.n_split + std::max(p.own_few.n_split, p.own_many.n_split));
+  const int n_own = std::max(p.own_few.n_split, p.own_many.n_split);
+  p.records = rows * (p.prefix.n_split + n_own);
+  // Against gear_page_attn, whose repeated reads of the shared pages the caches serve: 0.04 ns per sequence, KV head and key with few columns (64 sequences of 8300 to 9200 tokens, 8 heads,
+  // 174 us, 16 of 2100, 32 heads, 44), 2.36 us per tile of 128 columns and 64 keys on 512 places with many (16 of 6150, 20 to 60 new tokens, 32 query heads over 8: 125 us, shared 97).
+  const double shared = parts.time + 4000.0 + record_bytes * n_own * 2.0 / 5000.0;
+  const double keys = (prefix * filled + 0.6 * own) * (double)b.n_seqs * H;
+  const double by_itself = all_few ? 7000.0 + 0.04 * (p.own_few.few <= 16 ? 1.0 : 1.4) * keys
+                                   : 8000.0 + keys / MANY_KEYS * std::ceil((double)all_cols / b.n_seqs / MANY_COLS) * 2360.0 * codes / MANY_SLOTS;
+  p.shared = gr.always != 0 || shared < by_itself;
   return p;
 }
 
@@ -56,7 +91,7 @@ using namespace gear;
 namespace {
 
 int check_groups(const gear_page_groups* g) {
-  if (!g || g->n_groups < 0 || g->max_q < 0 || g->max_prefix < 0) return GEAR_EINVAL;
+  if (!g || g->n_groups < 0 || g->max_q < 0 || g->max_prefix < 0 || (g->always != 0 && g->always != 1)) return GEAR_EINVAL;
   return GEAR_OK;
 }
 

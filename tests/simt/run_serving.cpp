@@ -143,6 +143,7 @@ int main(int, char** argv) {
       b.kv_len = at<int32_t>(f);
       b.page_table = at<int32_t>(f);
       f >> g.n_groups >> g.max_q >> g.max_prefix;
+      g.always = 1;
       g.group_start = at<int32_t>(f);
       g.prefix_len = at<int32_t>(f);
       const gear_page_rows *q = view(f), *out = view(f);

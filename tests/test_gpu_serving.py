@@ -236,12 +236,12 @@ class Batch:
         self.T = self.q_start[-1] + pad
         self.q = torch.randn(self.T, H * gq, 128, generator=gen).to(dtype)
 
-    def made(self, causal=True, prefix=None, table=None, max_prefix=None):
+    def made(self, causal=True, prefix=None, table=None, max_prefix=None, always=True):
         most = max(self.q_start[b] - self.q_start[a] for a, b in zip(self.group_start, self.group_start[1:]))
         prefix = self.prefix if prefix is None else prefix
         b = gb.make_page_batch(i32(self.q_start), i32(self.kv), (self.table if table is None else table).to(DEV), self.T,
                                max(b - a for a, b in zip(self.q_start, self.q_start[1:])), max(self.kv), causal)
-        return b, gb.make_page_groups(i32(self.group_start), i32(prefix), most, max(prefix) if max_prefix is None else max_prefix)
+        return b, gb.make_page_groups(i32(self.group_start), i32(prefix), most, max(prefix) if max_prefix is None else max_prefix, always)
 
     def run(self, q=None, out=None, scale=128 ** -0.5, made=None, **kw):
         b, g = made or self.made(**kw)
@@ -284,6 +284,7 @@ def test_shared_prefixes(form, shape):
     c = Batch(dtype, bits, group, page, H, gq, groups, pad, seed=shape)
     for causal in (True, False):
         c.check(c.run(causal=causal), causal=causal)
+    c.check(c.run(always=False))
 
 
 @pytest.mark.parametrize("form", [FORMS[0], FORMS[3], FORMS[4]], ids=lambda f: "%s-%d-%d" % (str(f[0])[6:], f[1], f[2]))
@@ -388,7 +389,7 @@ class Served:
         at = i32(rows).long()
         b = gb.make_page_batch(i32([n * i for i in range(len(rows) + 1)]), self.t.kv_len[at], self.t.table[at].contiguous(), n * len(rows), n, max(len(self.rows[r]) for r in rows))
         start, prefix = groups
-        g = gb.make_page_groups(i32(start), i32(prefix), n * max(b - a for a, b in zip(start, start[1:])), max(prefix))
+        g = gb.make_page_groups(i32(start), i32(prefix), n * max(b - a for a, b in zip(start, start[1:])), max(prefix), always=True)
         return self.pool.attn_shared(q, b, g)
 
 
@@ -458,7 +459,7 @@ def test_a_step_is_captured_and_replayed():
         gb.gear_page_move(s.cfg, s.pool.pool, copies)
         gb.gear_page_write_rope(s.cfg, s.pool.pool, s.rope, qkv[:, :, 8:10], qkv[:, :, 10:], slots, pos, qkv[:, :, :8], q_out)
         b = gb.make_page_batch(q_start, s.t.kv_len[1:7], s.t.table[1:7], 12, 2, 400)
-        gb.gear_page_attn_shared(s.cfg, s.pool.pool, b, gb.make_page_groups(start, prefix, 12, 130), q_out.view(12, 8, 128), out, 128 ** -0.5, ws)
+        gb.gear_page_attn_shared(s.cfg, s.pool.pool, b, gb.make_page_groups(start, prefix, 12, 130, always=True), q_out.view(12, 8, 128), out, 128 ** -0.5, ws)
         gb.gear_page_truncate(s.t.c, dst, zero)
         return b
 

@@ -48,13 +48,13 @@ def batch(**kw):
 
 
 def groups(**kw):
-    return changed(gb.gear_page_groups(2, 7, 80, FAKE, FAKE), **kw)
+    return changed(gb.gear_page_groups(2, 7, 80, 1, FAKE, FAKE), **kw)
 
 
 def test_struct_sizes_match_header():
     assert ctypes.sizeof(gb.gear_rope) == 4 * 4 + 8
     assert ctypes.sizeof(gb.gear_page_table) == 4 * 4 + 3 * 8
-    assert ctypes.sizeof(gb.gear_page_groups) == 3 * 4 + 4 + 2 * 8
+    assert ctypes.sizeof(gb.gear_page_groups) == 4 * 4 + 2 * 8
 
 
 def test_frequencies(lib):
@@ -186,7 +186,7 @@ def test_shared_attention_is_checked(lib):
     assert call(q=None) == INVAL and call(out=None) == INVAL and call(H_q=6) == INVAL and call(scale=float("nan")) == INVAL
     for kw in (dict(n_seqs=-1), dict(n_tokens=-1), dict(max_q=-1), dict(max_kv=-1), dict(table_width=-1), dict(q_start=None), dict(kv_len=None), dict(page_table=None)):
         assert call(b=batch(**kw)) == INVAL, kw
-    for kw in (dict(n_groups=-1), dict(max_q=-1), dict(max_prefix=-1), dict(group_start=None), dict(prefix_len=None)):
+    for kw in (dict(n_groups=-1), dict(max_q=-1), dict(max_prefix=-1), dict(always=2), dict(always=-1), dict(group_start=None), dict(prefix_len=None)):
         assert call(g=groups(**kw)) == INVAL, kw
     for kw in (dict(group_start=FAKE + 2), dict(prefix_len=FAKE + 1)):
         assert call(g=groups(**kw)) == ALIGN, kw
