@@ -382,7 +382,7 @@ int gear_page_write_rope(const gear_page_config* cfg, void* pool, size_t pool_by
  * Rows outside 0 .. n_rows - 1 in a list are passed over.  The calls on one table must be ordered on one stream.
  */
 typedef struct gear_page_table {
-  int32_t n_pages;     /* pages of a pool, 1 .. 2^27                       */
+  int32_t n_pages;     /* pages of a pool, 1 .. 2^20                       */
   int32_t page_size;   /* tokens per page: 16, 32, 64, 128 or 256          */
   int32_t n_rows;      /* sequences, 1 .. 2^18                             */
   int32_t width;       /* entries of a row, width * page_size below 2^31   */

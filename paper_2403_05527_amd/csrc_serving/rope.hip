@@ -107,15 +107,6 @@ __device__ __forceinline__ uint4 turned(const Rope& r, const LaneTurns& t, const
   return make_uint4(turn_pair<BF>(v.x, o.x, t, 0), turn_pair<BF>(v.y, o.y, t, 2), turn_pair<BF>(v.z, o.z, t, 4), turn_pair<BF>(v.w, o.w, t, 6));
 }
 
-// (rows that are read once need no place in the caches: 2 us of 184 where 8-bit pages are written)
-__device__ __forceinline__ uint4 load16_once(const unsigned char* p) {
-#ifdef GEAR_NO_NONTEMPORAL
-  return *reinterpret_cast<const uint4*>(p);
-#else
-  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p)));
-#endif
-}
-
 // grid: (part of the heads, 16 tokens of one sequence).  BITS: of the pool's rows, 0 where there is none.  A block has up to HEADS heads at a time on their way.
 // PAST: `out` is large (PAST_CACHES).  (As a branch at the store it was lost: both stores became one.)
 constexpr int HEADS = 8;

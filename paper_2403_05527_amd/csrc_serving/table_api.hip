@@ -6,7 +6,7 @@ using namespace gear;
 
 namespace {
 
-constexpr int PAGES_MOST = 1 << 27, ROWS_MOST = 1 << 18;
+constexpr int PAGES_MOST = 1 << 20, ROWS_MOST = 1 << 18;
 
 int check_table(const gear_page_table* t, int64_t n, PageTable* to) {
   if (!t || n < 0) return GEAR_EINVAL;

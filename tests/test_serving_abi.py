@@ -151,7 +151,7 @@ def test_tables_are_checked(lib):
             assert call(t=table(**kw)) == INVAL, kw
         for kw in (dict(table=FAKE + 2), dict(kv_len=FAKE + 1), dict(refs=FAKE + 4)):
             assert call(t=table(**kw)) == ALIGN, kw
-        for kw in (dict(n_pages=(1 << 27) + 1), dict(n_rows=(1 << 18) + 1), dict(width=1 << 27)):
+        for kw in (dict(n_pages=(1 << 20) + 1), dict(n_rows=(1 << 18) + 1), dict(width=1 << 27)):
             assert call(t=table(**kw)) == CAP, kw
     for call in (extend, truncate, fork):
         assert call(r=None) == INVAL and call(c=None) == INVAL and call(r=FAKE + 2) == ALIGN and call(c=FAKE + 1) == ALIGN
