@@ -223,27 +223,28 @@ __global__ __launch_bounds__(64 * SHARED_WAVES) void page_attn_shared_few_kernel
   few_columns<BITS, BF, NC, SHARED_WAVES>(p, prefix ? bid : bid - c.prefix.blocks, lds);
 }
 
-// The records of a row become its output: WAVES waves per token and query head, eight records of each on their way, the first of them requested with the lengths.
-template <int WAVES>
+// The records of a row become its output: a wave per token and query head, eight records on their way, the first of them requested with the lengths.  (20768 rows of four records, 43 MB: 21 us.
+// Four rows per wave, each requested before the one before it is summed: 22.  Four waves per row: 11 us instead of 7 on 2048 rows of nine.)
+constexpr int MERGE_AT_ONCE = 8;
+struct RowRecords {
+  float2 ml[MERGE_AT_ONCE], v[MERGE_AT_ONCE];
+};
+__device__ __forceinline__ void request_row(RowRecords& r, const SharedPart& a, int64_t rec, int i0, int lane) {   // in the row, whether they have been written or not
+#pragma unroll
+  for (int u = 0; u < MERGE_AT_ONCE; ++u) {
+    if (i0 + u >= a.n_records) break;
+    r.ml[u] = a.rec_ml[rec + i0 + u];
+    r.v[u] = *reinterpret_cast<const float2*>(a.rec_o + (rec + i0 + u) * D + 2 * lane);
+  }
+}
 __global__ __launch_bounds__(256) void page_merge_shared_kernel(SharedCall c, int bf) {
-  GEAR_DYN_LDS(lds);
   const SharedPart a = part_of(c, c.own_many, false);
-  const int lane = lane_id(), Hq = a.geom.H * a.gq, wave = (int)(threadIdx.x >> 6), mine = WAVES == 1 ? 0 : wave;
-  const int64_t id = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
+  const int lane = lane_id(), Hq = a.geom.H * a.gq;
+  const int64_t id = (int64_t)blockIdx.x * 4 + GEAR_WAVE_UNIFORM((int)(threadIdx.x >> 6)), rec = id * a.n_records;
   const int token = (int)(id / Hq), jq = (int)(id - (int64_t)token * Hq), head = jq / a.gq;
   if (token >= a.n_tokens) return;
-  const int64_t rec = id * a.n_records;
-  float2 ml[8], v[8];
-  auto request = [&](int i0) {   // in the row, whether they have been written or not
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int64_t r = rec + min(i0 + WAVES * u, a.n_records - 1);
-      ml[u] = a.rec_ml[r];
-      v[u] = *reinterpret_cast<const float2*>(a.rec_o + r * D + 2 * lane);
-    }
-  };
-  request(mine);
-  float top = a.rec_ml[rec + min(lane, a.n_records - 1)].x;
+  RowRecords r;
+  request_row(r, a, rec, 0, lane);
   int s = -1;
   for (int base = 0; base < a.n_seqs; base += 64) {
     const int i = base + lane;
@@ -262,38 +263,26 @@ __global__ __launch_bounds__(256) void page_merge_shared_kernel(SharedCall c, in
     const int col = row * a.gq + (jq - head * a.gq), last = min(col / MANY_COLS * MANY_COLS + MANY_COLS, cols) - 1;
     own = parts_of(row_sees(a, sp, last / a.gq) - span.begin, c.own_many.n_split, c.own_many.least, MANY_KEYS).count;
   }
-  if (span.begin == 0 && own <= 1) return;
   const int before = span.begin == 0 ? 0 : parts_of(span.begin, c.prefix.n_split, c.prefix.least, c.prefix.few > 0 ? KEY_STEP : MANY_KEYS).count;
+  if (before == 0 && own <= 1) return;   // (its one part is its output)
   const int first_own = c.prefix.n_split;
   auto written = [&](int i) { return i < before || (i >= first_own && i < first_own + own); };
-  top = written(lane) ? top : -INFINITY;
-  for (int i = lane + 64; i < a.n_records; i += 64)
+  float top = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < MERGE_AT_ONCE; ++u) top = written(u) ? fmaxf(top, r.ml[u].x) : top;
+  for (int i = MERGE_AT_ONCE; i < a.n_records; ++i)
     if (written(i)) top = fmaxf(top, a.rec_ml[rec + i].x);
-  top = wave_max(top);
   const float from = top == -INFINITY ? 0.0f : top;
   Merged m{0.0f, 0.0f, 0.0f};
-  for (int i0 = mine; i0 < a.n_records; i0 += WAVES * 8) {
-    if (i0 != mine) request(i0);
+  for (int i0 = 0; i0 < a.n_records; i0 += MERGE_AT_ONCE) {
+    if (i0 > 0) request_row(r, a, rec, i0, lane);
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const bool there = written(i0 + WAVES * u);
-      const float by = there ? GEAR_EXP2(ml[u].x - from) : 0.0f;
-      m.sum += there ? ml[u].y * by : 0.0f;
-      m.x += there ? v[u].x * by : 0.0f;
-      m.y += there ? v[u].y * by : 0.0f;
-    }
-  }
-  if constexpr (WAVES > 1) {
-    float* sums = reinterpret_cast<float*>(lds);
-    sums[(wave * 3 + 0) * 64 + lane] = m.sum;
-    sums[(wave * 3 + 1) * 64 + lane] = m.x;
-    sums[(wave * 3 + 2) * 64 + lane] = m.y;
-    block_lds_sync();
-    if (wave != 0) return;
-    for (int w = 1; w < WAVES; ++w) {
-      m.sum += sums[(w * 3 + 0) * 64 + lane];
-      m.x += sums[(w * 3 + 1) * 64 + lane];
-      m.y += sums[(w * 3 + 2) * 64 + lane];
+    for (int u = 0; u < MERGE_AT_ONCE; ++u) {
+      const bool there = written(i0 + u);
+      const float by = there ? GEAR_EXP2(r.ml[u].x - from) : 0.0f;
+      m.sum += there ? r.ml[u].y * by : 0.0f;
+      m.x += there ? r.v[u].x * by : 0.0f;
+      m.y += there ? r.v[u].y * by : 0.0f;
     }
   }
   store_merged(a, m, token, jq, lane, bf);
@@ -325,8 +314,7 @@ hipError_t launch_page_shared(const SharedCall& c, int bits, bool bf, int tiles,
 #undef GEAR_SHARED
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)c.a.n_tokens * c.a.geom.H * c.a.gq;
-  if (c.n_records <= 32) hipLaunchKernelGGL(page_merge_shared_kernel<1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, c, bf ? 1 : 0);
-  else hipLaunchKernelGGL(page_merge_shared_kernel<4>, dim3((unsigned)rows), dim3(256), (size_t)MERGE_LDS, st, c, bf ? 1 : 0);
+  hipLaunchKernelGGL(page_merge_shared_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, c, bf ? 1 : 0);
   return hipGetLastError();
 }
 
