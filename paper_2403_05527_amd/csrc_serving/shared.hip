@@ -16,6 +16,7 @@ struct SharedPart : PageAttn {
   const int32_t* group_start;
   const int32_t* prefix_len;
   int32_t n_groups, n_records, first_record;
+  int32_t group_cols;   // columns up to which a group has its prefix read; 0: any number
   bool prefix;
 };
 
@@ -54,7 +55,10 @@ __device__ __forceinline__ Lanes load_lanes(const SharedPart& a, int lane) {
 __device__ __forceinline__ SeqSpan lane_span(const Lanes& l, int s) {
   return SeqSpan{__builtin_amdgcn_readlane(l.sp.q0, s), __builtin_amdgcn_readlane(l.sp.nq, s), __builtin_amdgcn_readlane(l.sp.kv, s)};
 }
+// (a group of more columns than the call's bound shares nothing, and is right all the same)
+__device__ __forceinline__ bool too_wide(const SharedPart& a, int rows) { return a.group_cols > 0 && (rows > a.group_cols || rows * a.gq > a.group_cols); }
 __device__ __forceinline__ int lane_keys(const SharedPart& a, const Lanes& l, int lane, int g, int s0, int s1) {
+  if (s1 <= s0 || too_wide(a, __builtin_amdgcn_readlane(l.sp.q0 + l.sp.nq, s1 - 1) - __builtin_amdgcn_readlane(l.sp.q0, s0))) return 0;
   const int least = wave_least(lane >= s0 && lane < s1 ? keys_before(a, l.sp) : INT_MAX);
   return whole_tiles(min(least, __builtin_amdgcn_readlane(l.len, g)));
 }
@@ -66,7 +70,15 @@ __device__ __forceinline__ int lane_before(const SharedPart& a, const Lanes& l, 
 }
 
 // The same from memory, for any number of them.
+__device__ __forceinline__ SeqSpan group_rows(const SharedPart& a, int s0, int s1) {   // a group's columns are those of its sequences, one behind the other (kv: not set)
+  SeqSpan r{0, 0, 0};
+  if (s1 <= s0) return r;
+  r.q0 = max(a.q_start[s0], 0);
+  r.nq = min(max(a.q_start[s1], 0), a.n_tokens) - r.q0;
+  return r;
+}
 __device__ __forceinline__ int shared_keys(const SharedPart& a, int g, int s0, int s1) {   // the prefix of group g, as far as it counts
+  if (too_wide(a, group_rows(a, s0, s1).nq)) return 0;
   int least = INT_MAX;
   for (int base = s0; base < s1; base += 64) {
     const int s = base + lane_id();
@@ -102,14 +114,6 @@ __device__ __forceinline__ int few_sequence(const SharedPart& a, int i) {
   return GEAR_WAVE_UNIFORM(__ffsll((long long)__ballot(lane < a.n_seqs && before == i)) - 1);
 }
 
-// A group's columns are those of its sequences, one behind the other.
-__device__ __forceinline__ SeqSpan group_rows(const SharedPart& a, int s0, int s1) {   // (kv: not set)
-  SeqSpan r{0, 0, 0};
-  if (s1 <= s0) return r;
-  r.q0 = max(a.q_start[s0], 0);
-  r.nq = min(max(a.q_start[s1], 0), a.n_tokens) - r.q0;
-  return r;
-}
 __device__ __forceinline__ Span span_of(const SharedPart& a, int s) {
   Span r;
   if (fits_lanes(a)) {
@@ -182,6 +186,7 @@ __device__ __forceinline__ SharedPart part_of(const SharedCall& c, const SharedK
   p.n_groups = c.n_groups;
   p.n_records = c.n_records;
   p.first_record = prefix ? 0 : c.prefix.n_split;
+  p.group_cols = c.prefix.few;
   p.prefix = prefix;
   p.n_split = k.n_split;
   p.least = k.least;
@@ -259,6 +264,8 @@ __global__ __launch_bounds__(256) void page_merge_shared_kernel(SharedCall c, in
   int own;
   if (sp.nq <= c.own_few.few && cols <= c.own_few.few) {
     own = parts_of(sp.kv - span.begin, c.own_few.n_split, c.own_few.least, KEY_STEP).count;
+  } else if (c.own_many.blocks == 0) {
+    return;   // (more new tokens than the call's bound: the rows stay)
   } else {
     const int col = row * a.gq + (jq - head * a.gq), last = min(col / MANY_COLS * MANY_COLS + MANY_COLS, cols) - 1;
     own = parts_of(row_sees(a, sp, last / a.gq) - span.begin, c.own_many.n_split, c.own_many.least, MANY_KEYS).count;

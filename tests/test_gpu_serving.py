@@ -308,6 +308,25 @@ def test_prefixes_that_are_not_what_the_call_says(form):
     c.check(c.run(table=gone), table=gone)
 
 
+def test_more_rows_than_the_call_says():
+    """A group of more rows than its bound is right all the same; a sequence of more new tokens than the batch's bound may stay as it was, and the others are right."""
+    c = Batch(F16, 16, 128, 16, 2, 4, [(300, [(1, 30)] * 6), (200, [(2, 9)] * 2)], seed=11)
+    b, g = c.made()
+    g.max_q = 2
+    c.check(c.run(made=(b, g)))
+    c = Batch(F16, 16, 128, 16, 2, 4, [(300, [(1, 30), (20, 30), (1, 1)]), (200, [(2, 9)] * 2)], seed=12)
+    b, g = c.made()
+    b.max_q = 2
+    out = c.run(made=(b, g)).cpu()
+    whole = c.run().cpu()
+    c.check(whole)
+    late = torch.zeros(c.T, dtype=torch.bool)
+    late[1:21] = True
+    assert bool((out[late] == 77.0).all()) or sv.is_close(out[late], whole[late].double(), torch.full_like(whole[late], 0.02).double()) <= 1.0
+    want, bound = pg.attend(c.q, c.K, c.V, c.q_start, c.kv, c.table.tolist(), 128 ** -0.5, True)
+    assert sv.is_close(out[~late], want[~late], bound[~late]) <= 1.0
+
+
 def test_slots_without_a_token_may_hold_anything():
     c = Batch(F16, 16, 128, 16, 2, 4, [(150, [(1, 30), (1, 1), (2, 9)] * 3), (70, [(1, 5)] * 2)], seed=4)
     held = torch.zeros(c.cfg.n_pages, 16, dtype=torch.bool)
