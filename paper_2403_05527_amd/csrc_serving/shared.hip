@@ -228,28 +228,32 @@ __global__ __launch_bounds__(64 * SHARED_WAVES) void page_attn_shared_few_kernel
   few_columns<BITS, BF, NC, SHARED_WAVES>(p, prefix ? bid : bid - c.prefix.blocks, lds);
 }
 
-// The records of a row become its output: a wave per token and query head, eight records on their way, the first of them requested with the lengths.  (20768 rows of four records, 43 MB: 21 us.
-// Four rows per wave, each requested before the one before it is summed: 22.  Four waves per row: 11 us instead of 7 on 2048 rows of nine.)
-constexpr int MERGE_AT_ONCE = 8;
+// The records of a row become its output: a wave per ROWS query heads of a token, ONCE records of each requested with the lengths, the others by as many.  Bound by its chain of
+// loads, 5 us for a wave, so that many rows go four to a wave: 20768 rows of four records, 43 MB, a wave per row 20 us, four rows 14.  (Four waves per row: 11 us instead of 7 on 2048 rows of
+// nine.)
+template <int ONCE>
 struct RowRecords {
-  float2 ml[MERGE_AT_ONCE], v[MERGE_AT_ONCE];
+  float2 ml[ONCE], v[ONCE];
 };
-__device__ __forceinline__ void request_row(RowRecords& r, const SharedPart& a, int64_t rec, int i0, int lane) {   // in the row, whether they have been written or not
+template <int ONCE>
+__device__ __forceinline__ void request_row(RowRecords<ONCE>& r, const SharedPart& a, int64_t rec, int i0, int lane) {   // in the row, whether they have been written or not
 #pragma unroll
-  for (int u = 0; u < MERGE_AT_ONCE; ++u) {
-    if (i0 + u >= a.n_records) break;
-    r.ml[u] = a.rec_ml[rec + i0 + u];
-    r.v[u] = *reinterpret_cast<const float2*>(a.rec_o + (rec + i0 + u) * D + 2 * lane);
+  for (int u = 0; u < ONCE; ++u) {
+    const int64_t i = rec + min(i0 + u, a.n_records - 1);
+    r.ml[u] = a.rec_ml[i];
+    r.v[u] = *reinterpret_cast<const float2*>(a.rec_o + i * D + 2 * lane);
   }
 }
+template <int ROWS, int ONCE>
 __global__ __launch_bounds__(256) void page_merge_shared_kernel(SharedCall c, int bf) {
   const SharedPart a = part_of(c, c.own_many, false);
   const int lane = lane_id(), Hq = a.geom.H * a.gq;
-  const int64_t id = (int64_t)blockIdx.x * 4 + GEAR_WAVE_UNIFORM((int)(threadIdx.x >> 6)), rec = id * a.n_records;
-  const int token = (int)(id / Hq), jq = (int)(id - (int64_t)token * Hq), head = jq / a.gq;
+  const unsigned id = (blockIdx.x * 4 + (unsigned)GEAR_WAVE_UNIFORM((int)(threadIdx.x >> 6))) * ROWS;   // (rows: below 2^20)
+  const int token = (int)(id / (unsigned)Hq), jq0 = (int)(id - (unsigned)token * (unsigned)Hq);
   if (token >= a.n_tokens) return;
-  RowRecords r;
-  request_row(r, a, rec, 0, lane);
+  RowRecords<ONCE> r[ROWS];
+#pragma unroll
+  for (int j = 0; j < ROWS; ++j) request_row(r[j], a, (int64_t)(id + j) * a.n_records, 0, lane);
   int s = -1;
   for (int base = 0; base < a.n_seqs; base += 64) {
     const int i = base + lane;
@@ -261,38 +265,41 @@ __global__ __launch_bounds__(256) void page_merge_shared_kernel(SharedCall c, in
   const SeqSpan& sp = span.sp;
   const int row = token - sp.q0, cols = sp.nq * a.gq;
   if (row < 0 || row >= sp.nq) return;
-  int own;
-  if (sp.nq <= c.own_few.few && cols <= c.own_few.few) {
-    own = parts_of(sp.kv - span.begin, c.own_few.n_split, c.own_few.least, KEY_STEP).count;
-  } else if (c.own_many.blocks == 0) {
-    return;   // (more new tokens than the call's bound: the rows stay)
-  } else {
-    const int col = row * a.gq + (jq - head * a.gq), last = min(col / MANY_COLS * MANY_COLS + MANY_COLS, cols) - 1;
-    own = parts_of(row_sees(a, sp, last / a.gq) - span.begin, c.own_many.n_split, c.own_many.least, MANY_KEYS).count;
-  }
+  const bool few = sp.nq <= c.own_few.few && cols <= c.own_few.few;
+  if (!few && c.own_many.blocks == 0) return;   // (more new tokens than the call's bound: the rows stay)
   const int before = span.begin == 0 ? 0 : parts_of(span.begin, c.prefix.n_split, c.prefix.least, c.prefix.few > 0 ? KEY_STEP : MANY_KEYS).count;
-  if (before == 0 && own <= 1) return;   // (its one part is its output)
+  // (of many columns, what lies behind a prefix is one part)
+  const int own = few && c.own_few.n_split > 1 ? parts_of(sp.kv - span.begin, c.own_few.n_split, c.own_few.least, KEY_STEP).count : 1;
+  if (before == 0 && own == 1) return;   // (their one part is their output)
   const int first_own = c.prefix.n_split;
   auto written = [&](int i) { return i < before || (i >= first_own && i < first_own + own); };
-  float top = -INFINITY;
 #pragma unroll
-  for (int u = 0; u < MERGE_AT_ONCE; ++u) top = written(u) ? fmaxf(top, r.ml[u].x) : top;
-  for (int i = MERGE_AT_ONCE; i < a.n_records; ++i)
-    if (written(i)) top = fmaxf(top, a.rec_ml[rec + i].x);
-  const float from = top == -INFINITY ? 0.0f : top;
-  Merged m{0.0f, 0.0f, 0.0f};
-  for (int i0 = 0; i0 < a.n_records; i0 += MERGE_AT_ONCE) {
-    if (i0 > 0) request_row(r, a, rec, i0, lane);
+  for (int j = 0; j < ROWS; ++j) {
+    const int64_t rec = (int64_t)(id + j) * a.n_records;
+    float top = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < MERGE_AT_ONCE; ++u) {
-      const bool there = written(i0 + u);
-      const float by = there ? GEAR_EXP2(r.ml[u].x - from) : 0.0f;
-      m.sum += there ? r.ml[u].y * by : 0.0f;
-      m.x += there ? r.v[u].x * by : 0.0f;
-      m.y += there ? r.v[u].y * by : 0.0f;
+    for (int u = 0; u < ONCE; ++u) top = written(u) ? fmaxf(top, r[j].ml[u].x) : top;
+    if (a.n_records > ONCE) {
+      float more = -INFINITY;
+      for (int i = ONCE + lane; i < a.n_records; i += 64)
+        if (written(i)) more = fmaxf(more, a.rec_ml[rec + i].x);
+      top = fmaxf(top, wave_max(more));
     }
+    const float from = top == -INFINITY ? 0.0f : top;
+    Merged m{0.0f, 0.0f, 0.0f};
+    for (int i0 = 0; i0 < a.n_records; i0 += ONCE) {
+      if (i0 > 0) request_row(r[j], a, rec, i0, lane);
+#pragma unroll
+      for (int u = 0; u < ONCE; ++u) {
+        const bool there = written(i0 + u);
+        const float by = there ? GEAR_EXP2(r[j].ml[u].x - from) : 0.0f;
+        m.sum += there ? r[j].ml[u].y * by : 0.0f;
+        m.x += there ? r[j].v[u].x * by : 0.0f;
+        m.y += there ? r[j].v[u].y * by : 0.0f;
+      }
+    }
+    store_merged(a, m, token, jq0 + j, lane, bf);
   }
-  store_merged(a, m, token, jq, lane, bf);
 }
 
 template <int BITS, bool BF, int NC>
@@ -314,6 +321,11 @@ static hipError_t launch_shared(const SharedCall& c, hipStream_t st) {
   return hipGetLastError();
 }
 
+#ifndef GEAR_MERGE_ROWS_MANY   // (the CPU stand-in lowers it)
+#define GEAR_MERGE_ROWS_MANY 4096
+#endif
+constexpr int64_t MERGE_ROWS_MANY = GEAR_MERGE_ROWS_MANY;   // rows from which on a wave has four of them
+
 hipError_t launch_page_shared(const SharedCall& c, int bits, bool bf, int tiles, hipStream_t st) {
 #define GEAR_SHARED(B) \
   (tiles == 1 ? (bf ? launch_shared<B, true, 1>(c, st) : launch_shared<B, false, 1>(c, st)) : (bf ? launch_shared<B, true, 2>(c, st) : launch_shared<B, false, 2>(c, st)))
@@ -321,7 +333,11 @@ hipError_t launch_page_shared(const SharedCall& c, int bits, bool bf, int tiles,
 #undef GEAR_SHARED
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)c.a.n_tokens * c.a.geom.H * c.a.gq;
-  hipLaunchKernelGGL(page_merge_shared_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, c, bf ? 1 : 0);
+  const dim3 blocks((unsigned)((rows + 3) / 4));
+  if (rows >= MERGE_ROWS_MANY && c.a.geom.H * c.a.gq % 4 == 0 && c.n_records <= 4)   // (four rows of a wave are one token's)
+    hipLaunchKernelGGL((page_merge_shared_kernel<4, 4>), dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, st, c, bf ? 1 : 0);
+  else if (c.n_records <= 8) hipLaunchKernelGGL((page_merge_shared_kernel<1, 8>), blocks, dim3(256), 0, st, c, bf ? 1 : 0);
+  else hipLaunchKernelGGL((page_merge_shared_kernel<1, 16>), blocks, dim3(256), 0, st, c, bf ? 1 : 0);
   return hipGetLastError();
 }
 

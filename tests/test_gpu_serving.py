@@ -272,6 +272,7 @@ GROUPS = [
     (16, 1, 3, [(64 + g % 3, [(1, 2 + g % 4)] * (1 + (g % 2))) for g in range(70)], 0),      # more groups than a wave has lanes
     (16, 1, 17, [(64 + g, [(1, 2 + g % 4)] * (2 + (g % 3))) for g in range(66)], 0),
     (256, 1, 1, [(2048, [(1, 300)] * 130), (1, [(1, 5)] * 3)], 3),                           # more sequences
+    (16, 2, 4, [(130, [(40, 45)] * 16)], 0),                                                 # many rows to join
     (16, 4, 1, [(129, [(300, 300), (1, 1)])], 0),                                            # a prompt: by itself
 ]
 
