@@ -434,14 +434,14 @@ int gear_page_move(const gear_page_config* cfg, void* pool, size_t pool_bytes, i
  * parts of a row's softmax are joined.  The same batch, and up to the order of sums the same result, as gear_page_attn.
  */
 typedef struct gear_page_groups {
-  int32_t n_groups;
+  int32_t n_groups;             /* up to 2^20                                                          */
   int32_t max_q;                /* no group has more rows of q (the rows of one that has may stay)     */
   int32_t max_prefix;           /* about the longest prefix: what the work is divided by               */
   int32_t always;               /* 0: prefixes are shared where that is estimated to be faster, else the call is gear_page_attn's; */
                                 /* 1: always (but where a workspace of 512 MB would not do)            */
   const int32_t* group_start;   /* device [n_groups + 1], ascending: group i has sequences group_start[i] .. */
-  const int32_t* prefix_len;    /* device [n_groups]: the first tokens that are the same in all of them; they are read through the
-                                 * group's first sequence's row of the page table.  Where the sequences part within a page, each may have its own copy. */
+  const int32_t* prefix_len;    /* device [n_groups]: the first tokens that are the same in all of them; they are read through the row
+                                 * of the page table of the group's first sequence that has new tokens.  Where the sequences part within a page, each may have its own copy. */
 } gear_page_groups;
 
 /* Workspace of gear_page_attn_shared for H_q query heads and every batch and groups with at most these n_seqs, n_tokens, max_q and max_kv, n_groups, max_q and

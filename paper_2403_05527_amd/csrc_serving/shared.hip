@@ -3,6 +3,9 @@
 // softmax over [prefix, own] is joined from parts: each part of the keys leaves its maximum, its sum of weights and its weighted sum of Values, and the parts are
 // brought to the greatest maximum.  The parts of a prefix take the columns of all the group's new tokens as one sequence's, with the keys that all of them see,
 // so a page is read once for 128 columns (32 in the kernel of few); what a sequence has behind the prefix is read as in gear_page_attn.  Both kinds of block run in one launch.
+// Bound by the matrix cores and exponentials of the prefix's tiles (questions about 6100 tokens, 2596 columns per KV head: 83 us, matrix cores 0.43 busy), by the bytes of what lies behind (64 sequences
+// of 100 to 1000 tokens behind 8192, 188 MB: 50 us), or, where both are small, by a block's chain of loads and joins (16 samples behind 2077 tokens, 32 heads: 13 us); and by the records, 520 bytes per
+// row and part, which the joining reads back.
 // A prefix counts to the last whole 64 tokens that every new token of the group sees, so that no key of it is masked from anyone; what is left of it is read with
 // each sequence's own tokens.
 #include "page_few.h"
@@ -121,18 +124,25 @@ __device__ __forceinline__ Span span_of(const SharedPart& a, int s) {
     const Lanes l = load_lanes(a, lane);
     if (!a.prefix) return Span{lane_span(l, s), lane_before(a, l, lane, s), s};
     const int s0 = __builtin_amdgcn_readlane(l.start, s), s1 = __builtin_amdgcn_readlane(l.start, s + 1);
-    r = Span{SeqSpan{0, 0, 0}, 0, s0};
-    if (s1 > s0) {
+    r = Span{SeqSpan{0, 0, 0}, 0, -1};
+    const unsigned long long rows = __ballot(lane >= s0 && lane < s1 && l.sp.nq > 0);
+    if (rows != 0ull) {
+      r.table_row = GEAR_WAVE_UNIFORM(__ffsll((long long)rows) - 1);   // the first that has new tokens: one without may have been freed
       const SeqSpan first = lane_span(l, s0), last = lane_span(l, s1 - 1);
       r.sp = SeqSpan{first.q0, last.q0 + last.nq - first.q0, lane_keys(a, l, lane, s, s0, s1)};
     }
   } else {
     if (!a.prefix) return Span{seq_span(a, s), shared_before(a, s), s};
     const int s0 = group_bound(a, s), s1 = group_bound(a, s + 1);
-    r = Span{group_rows(a, s0, s1), 0, s0};
-    if (r.sp.nq > 0) r.sp.kv = shared_keys(a, s, s0, s1);
+    r = Span{group_rows(a, s0, s1), 0, -1};
+    for (int base = s0; base < s1 && r.table_row < 0; base += 64) {
+      const int i = base + lane_id();
+      const unsigned long long rows = __ballot(i < s1 && seq_span(a, min(i, a.n_seqs - 1)).nq > 0);
+      if (rows != 0ull) r.table_row = GEAR_WAVE_UNIFORM(base + __ffsll((long long)rows) - 1);
+    }
+    if (r.table_row >= 0 && r.sp.nq > 0) r.sp.kv = shared_keys(a, s, s0, s1);
   }
-  if (r.sp.kv == 0) r.sp.nq = 0;
+  if (r.table_row < 0 || r.sp.kv == 0) r.sp.nq = 0;
   return r;
 }
 __device__ __forceinline__ bool is_output(const SharedPart& a, const Span& span, int parts) { return !a.prefix && span.begin == 0 && parts == 1; }

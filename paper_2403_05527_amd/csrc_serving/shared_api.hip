@@ -90,9 +90,11 @@ using namespace gear;
 
 namespace {
 
+constexpr int GROUPS_MOST = 1 << 20;
+
 int check_groups(const gear_page_groups* g) {
   if (!g || g->n_groups < 0 || g->max_q < 0 || g->max_prefix < 0 || (g->always != 0 && g->always != 1)) return GEAR_EINVAL;
-  return GEAR_OK;
+  return g->n_groups > GROUPS_MOST ? GEAR_ECAPACITY : GEAR_OK;
 }
 
 }  // namespace

@@ -309,6 +309,15 @@ def test_prefixes_that_are_not_what_the_call_says(form):
     c.check(c.run(table=gone), table=gone)
 
 
+@pytest.mark.parametrize("more", (0, 70))
+def test_the_first_sequence_of_a_group_may_be_an_empty_place(more):
+    """A row of the batch that has been freed: no tokens, no pages, no new ones; the prefix is read through the others' rows."""
+    c = Batch(F16, 16, 128, 16, 2, 4, [(200, [(0, 4), (1, 5), (2, 9), (0, 3)]), (0, [(0, 0)]), (300, [(0, 1), (0, 1)])] + [(0, [(1, 3)])] * more, seed=13)
+    for s in (0, 5, 6):
+        c.table[s], c.kv[s] = -1, 0
+    c.check(c.run())
+
+
 def test_more_rows_than_the_call_says():
     """A group of more rows than its bound is right all the same; a sequence of more new tokens than the batch's bound may stay as it was, and the others are right."""
     c = Batch(F16, 16, 128, 16, 2, 4, [(300, [(1, 30)] * 6), (200, [(2, 9)] * 2)], seed=11)

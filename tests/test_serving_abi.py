@@ -191,6 +191,7 @@ def test_shared_attention_is_checked(lib):
     for kw in (dict(group_start=FAKE + 2), dict(prefix_len=FAKE + 1)):
         assert call(g=groups(**kw)) == ALIGN, kw
     assert call(out=rows(token=0)) == INVAL and call(q=rows(FAKE + 2)) == ALIGN and call(ws=FAKE + 8, wn=1 << 30) == ALIGN and call(nbytes=n - 1) == CAP
+    assert call(g=groups(n_groups=(1 << 20) + 1)) == CAP
     assert call(b=batch(n_seqs=1 << 25)) == CAP and call(b=batch(table_width=1 << 27)) == CAP
     need = gb.gear_page_attn_shared_bytes(cfg, 8, batch(), groups())
     assert need > 0 and call() == INVAL and call(ws=FAKE, wn=16) == CAP          # records of the parts need a workspace
