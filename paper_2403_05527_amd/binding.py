@@ -280,7 +280,7 @@ def _page_rows(t, cfg, heads, device, what):
 
 
 def _page_index(t, dtype, n, device, what):
-    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
         raise ValueError("%s is a contiguous %s tensor of %d entries: got %s %s" % (what, dtype, n, t.dtype, tuple(t.shape)))
     if t.get_device() != device:
         raise ValueError("%s lies on %s, not on the current GPU" % (what, t.device))
@@ -430,43 +430,41 @@ def make_page_table(table, kv_len, refs, page_size):
     return t
 
 
-def _table_lists(t, *lists):
-    """(addresses, entries) of int32 lists of one length."""
+def _table_device(t):
     device = _page_device()
     if getattr(t, "device", device) != device:
         raise ValueError("the page table lies on cuda:%d, not on the current GPU" % t.device)
-    n = lists[0][0].numel()
-    return [_page_index(x, torch.int32, n * per, device, what) for x, per, what in lists], n
+    return device
 
 
 def gear_page_extend(t, rows, counts, slots, copies, refused):
     """slots: int64 [n, max_count]; copies int32 [n, 2]; refused int32 [n]."""
-    (r, c, p, f), n = _table_lists(t, (rows, 1, "rows"), (counts, 1, "counts"), (copies, 2, "copies"), (refused, 1, "refused"))
-    if slots.dim() != 2 or slots.shape[0] != n:
-        raise ValueError("slots is [%d, max_count]: got %s" % (n, tuple(slots.shape)))
-    _check(load_library().gear_page_extend(t, r, c, n, slots.shape[1], _page_index(slots, torch.int64, slots.numel(), _page_device(), "slots"), p, f, _stream()),
-           "gear_page_extend")
+    d, n, shape = _table_device(t), rows.numel(), slots.shape
+    if len(shape) != 2 or shape[0] != n:
+        raise ValueError("slots is [%d, max_count]: got %s" % (n, tuple(shape)))
+    _check(load_library().gear_page_extend(t, _page_index(rows, torch.int32, n, d, "rows"), _page_index(counts, torch.int32, n, d, "counts"), n, shape[1],
+                                           _page_index(slots, torch.int64, n * shape[1], d, "slots"), _page_index(copies, torch.int32, 2 * n, d, "copies"),
+                                           _page_index(refused, torch.int32, n, d, "refused"), _stream()), "gear_page_extend")
 
 
 def gear_page_truncate(t, rows, lens):
-    (r, k), n = _table_lists(t, (rows, 1, "rows"), (lens, 1, "lens"))
-    _check(load_library().gear_page_truncate(t, r, k, n, _stream()), "gear_page_truncate")
+    d, n = _table_device(t), rows.numel()
+    _check(load_library().gear_page_truncate(t, _page_index(rows, torch.int32, n, d, "rows"), _page_index(lens, torch.int32, n, d, "lens"), n, _stream()),
+           "gear_page_truncate")
 
 
 def gear_page_fork(t, src, dst):
-    (a, b), n = _table_lists(t, (src, 1, "src"), (dst, 1, "dst"))
-    _check(load_library().gear_page_fork(t, a, b, n, _stream()), "gear_page_fork")
+    d, n = _table_device(t), src.numel()
+    _check(load_library().gear_page_fork(t, _page_index(src, torch.int32, n, d, "src"), _page_index(dst, torch.int32, n, d, "dst"), n, _stream()), "gear_page_fork")
 
 
 def gear_page_compact(t, moves, counts):
     """moves: int32 [max_moves, 2]; counts int32 [2]: pages in use, moves."""
+    d = _table_device(t)
     if moves.dim() != 2 or moves.shape[1] != 2:
         raise ValueError("moves is [max_moves, 2]: got %s" % (tuple(moves.shape),))
-    (c,), _ = _table_lists(t, (counts, 1, "counts"))
-    if counts.numel() != 2:
-        raise ValueError("counts has two entries: got %s" % (tuple(counts.shape),))
-    _check(load_library().gear_page_compact(t, _page_index(moves, torch.int32, moves.numel(), _page_device(), "moves"), moves.shape[0], c, _stream()),
-           "gear_page_compact")
+    _check(load_library().gear_page_compact(t, _page_index(moves, torch.int32, moves.numel(), d, "moves"), moves.shape[0],
+                                            _page_index(counts, torch.int32, 2, d, "counts"), _stream()), "gear_page_compact")
 
 
 def gear_page_move(cfg, pool, pairs):

@@ -184,6 +184,26 @@ def test_a_large_pool_and_a_full_list():
     assert counts.tolist() == [int((t.refs > 0).sum()), 0] and int((moves + 1).abs().sum()) == 0
 
 
+def test_the_largest_pool_is_compacted():
+    """2^20 pages (a bit each in the 160 KB of LDS), those in use at its end."""
+    n_pages = 1 << 20
+    t = gb.PageTable(n_pages, 16, 3, 400)
+    t.refs[:n_pages - 1000] = 1                              # (as if other tables had them, so that the rows get the last)
+    _, _, refused = t.extend(i32([2, 0]), i32([300 * 16, 5]), 300 * 16)
+    t.refs[:n_pages - 1000] = 0
+    t.refs[7] = 1                                            # one that is in its place, and one that is not named
+    before = t.table.clone()
+    moves, counts = t.compact(1000)
+    assert refused.tolist() == [0, 0] and counts.tolist() == [302, 301]
+    high = torch.arange(n_pages - 1000 + 300, n_pages - 1000 - 1, -1, device=DEV)
+    low = torch.tensor([p for p in range(302) if p != 7], device=DEV)
+    assert torch.equal(moves[:301].long(), torch.stack((high, low), 1)) and bool((moves[301:] == -1).all())
+    goes = torch.full((n_pages,), -1, dtype=torch.int32, device=DEV)
+    goes[high] = low.to(torch.int32)
+    assert torch.equal(t.table, torch.where(before >= 0, goes[before.clamp(min=0).long()], -1))
+    assert torch.equal(t.refs, (torch.arange(n_pages, device=DEV) < 302).to(torch.int32))
+
+
 def test_running_out_of_pages_changes_nothing_of_the_refused():
     t, m = gb.PageTable(8, 16, 6, 8), sv.Table(8, 16, 6, 8)
     for a, n in (([0], [20]), ([1, 2], [40, 40]), ([3], [1])):
