@@ -4,7 +4,7 @@
 // brought to the greatest maximum.  The parts of a prefix take the columns of all the group's new tokens as one sequence's, with the keys that all of them see,
 // so a page is read once for 128 columns (32 in the kernel of few); what a sequence has behind the prefix is read as in gear_page_attn.  Both kinds of block run in one launch.
 // Bound by the matrix cores and exponentials of the prefix's tiles (questions about 6100 tokens, 2596 columns per KV head: 83 us, matrix cores 0.43 busy), by the bytes of what lies behind (64 sequences
-// of 100 to 1000 tokens behind 8192, 188 MB: 50 us), or, where both are small, by a block's chain of loads and joins (16 samples behind 2077 tokens, 32 heads: 13 us); and by the records, 520 bytes per
+// of 100 to 1000 tokens behind 8192, 188 MB: 50 us), or, where both are small, by a block's chain of loads and joins (16 samples behind 2077 tokens, 32 heads: 12.7 us); and by the records, 520 bytes per
 // row and part, which the joining reads back.
 // A prefix counts to the last whole 64 tokens that every new token of the group sees, so that no key of it is masked from anyone; what is left of it is read with
 // each sequence's own tokens.
@@ -99,9 +99,9 @@ __device__ __forceinline__ int shared_before(const SharedPart& a, int s) {
   const int s0 = group_bound(a, g), s1 = group_bound(a, g + 1);
   return s < s1 ? shared_keys(a, g, s0, s1) : 0;
 }
-// What lies behind the prefixes, longest first: those that begin when the prefixes' blocks have ended are short.
+// What lies behind the prefixes, longest first: those that begin when the prefixes' blocks have ended are short.  (Not where all have few columns: four blocks to a CU, they mostly begin at once.)
 __device__ __forceinline__ int few_sequence(const SharedPart& a, int i) {
-  if (a.prefix || !fits_lanes(a)) return i;
+  if (a.prefix || a.group_cols > 0 || !fits_lanes(a)) return i;
   const int lane = lane_id();
   const Lanes l = load_lanes(a, lane);
   int own = lane < a.n_seqs ? l.sp.kv : -1;
