@@ -397,6 +397,7 @@ def gear_rotate(rope, x, out, positions):
 
 
 def gear_page_write_rope(cfg, pool, rope, K, V, slots, positions, q=None, q_out=None):
+    """Rows as gear_page_write takes them, and a position for each; q_out may be q."""
     device = _page_device()
     _rope_device(rope, device)
     if (q is None) != (q_out is None):
