@@ -129,7 +129,9 @@ constexpr size_t few_lds_bytes() {
 template <int BITS, bool BF, int NC, int WAVES, class Attn>
 __device__ __forceinline__ void few_columns(const Attn& a, int bid, unsigned char* lds) {
   const PageGeom& g = a.geom;
-  const int head = bid % g.H, rest = bid / g.H, part = rest % a.n_split, s = few_sequence(a, rest / a.n_split);
+  const int head = bid % g.H;
+  const Place place = few_place(a, bid / g.H);
+  const int part = place.part, s = place.i;
   const int lane = lane_id(), wave = GEAR_WAVE_UNIFORM((int)(threadIdx.x >> 6)), c = lane & 15, hh = lane >> 4;
   const Span span = span_of(a, s);
   const SeqSpan& sp = span.sp;

@@ -17,6 +17,7 @@ struct SharedCall {
   const int32_t* prefix_len;
   int32_t n_groups;
   int32_t n_records;      // parts of prefixes, then of what lies behind
+  int32_t usual_records;  // of most rows (SharedPlan)
   SharedKind prefix, own_many, own_few;   // few > 0 in `prefix`: by the kernel of few columns
 };
 
@@ -24,6 +25,7 @@ struct SharedPlan {
   bool shared;            // else the call is gear_page_attn's
   SharedKind prefix, own_many, own_few;   // blocks: not set
   int tiles;              // of 16 columns, of the kernel of few
+  int usual_records;      // of a row that has no more behind its prefix than the longest sequence has behind the longest prefix
   int64_t records;
 };
 

@@ -101,7 +101,7 @@ __device__ __forceinline__ int shared_before(const SharedPart& a, int s) {
 }
 // What lies behind the prefixes, longest first: those that begin when the prefixes' blocks have ended are short.  (Not where all have few columns: four blocks to a CU, they mostly begin at once.)
 __device__ __forceinline__ int few_sequence(const SharedPart& a, int i) {
-  if (a.prefix || a.group_cols > 0 || !fits_lanes(a)) return i;
+  if (a.group_cols > 0 || !fits_lanes(a)) return i;
   const int lane = lane_id();
   const Lanes l = load_lanes(a, lane);
   int own = lane < a.n_seqs ? l.sp.kv : -1;
@@ -115,6 +115,13 @@ __device__ __forceinline__ int few_sequence(const SharedPart& a, int i) {
     before += other > own || (other == own && j < lane) ? 1 : 0;
   }
   return GEAR_WAVE_UNIFORM(__ffsll((long long)__ballot(lane < a.n_seqs && before == i)) - 1);
+}
+
+// Of what lies behind the prefixes all first parts come first: few sequences have more, and the blocks of parts that are not there leave at the end.
+__device__ __forceinline__ Place few_place(const SharedPart& a, int at) {
+  if (a.prefix) return few_place(static_cast<const PageAttn&>(a), at);
+  const int part = a.n_split == 1 ? 0 : at / a.n_seqs;
+  return Place{few_sequence(a, at - part * a.n_seqs), part};
 }
 
 __device__ __forceinline__ Span span_of(const SharedPart& a, int s) {
@@ -279,25 +286,28 @@ __global__ __launch_bounds__(256) void page_merge_shared_kernel(SharedCall c, in
   if (!few && c.own_many.blocks == 0) return;   // (more new tokens than the call's bound: the rows stay)
   const int before = span.begin == 0 ? 0 : parts_of(span.begin, c.prefix.n_split, c.prefix.least, c.prefix.few > 0 ? KEY_STEP : MANY_KEYS).count;
   // (of many columns, what lies behind a prefix is one part)
-  const int own = few && c.own_few.n_split > 1 ? parts_of(sp.kv - span.begin, c.own_few.n_split, c.own_few.least, KEY_STEP).count : 1;
+  // (what rounds to one part is one)
+  const int behind = sp.kv - span.begin;
+  const bool divided = few && c.own_few.n_split > 1 && behind >= 2 * c.own_few.least - c.own_few.least / 2;
+  const int own = divided ? parts_of(behind, c.own_few.n_split, c.own_few.least, KEY_STEP).count : 1;
   if (before == 0 && own == 1) return;   // (their one part is their output)
-  const int first_own = c.prefix.n_split;
-  auto written = [&](int i) { return i < before || (i >= first_own && i < first_own + own); };
+  const int first_own = c.prefix.n_split, end = first_own + own;
+  auto written = [&](int i) { return i < before || (i >= first_own && i < end); };
 #pragma unroll
   for (int j = 0; j < ROWS; ++j) {
     const int64_t rec = (int64_t)(id + j) * a.n_records;
     float top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < ONCE; ++u) top = written(u) ? fmaxf(top, r[j].ml[u].x) : top;
-    if (a.n_records > ONCE) {
+    if (end > ONCE) {
       float more = -INFINITY;
-      for (int i = ONCE + lane; i < a.n_records; i += 64)
+      for (int i = ONCE + lane; i < end; i += 64)
         if (written(i)) more = fmaxf(more, a.rec_ml[rec + i].x);
       top = fmaxf(top, wave_max(more));
     }
     const float from = top == -INFINITY ? 0.0f : top;
     Merged m{0.0f, 0.0f, 0.0f};
-    for (int i0 = 0; i0 < a.n_records; i0 += ONCE) {
+    for (int i0 = 0; i0 < end; i0 += ONCE) {
       if (i0 > 0) request_row(r[j], a, rec, i0, lane);
 #pragma unroll
       for (int u = 0; u < ONCE; ++u) {
@@ -344,9 +354,9 @@ hipError_t launch_page_shared(const SharedCall& c, int bits, bool bf, int tiles,
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)c.a.n_tokens * c.a.geom.H * c.a.gq;
   const dim3 blocks((unsigned)((rows + 3) / 4));
-  if (rows >= MERGE_ROWS_MANY && c.a.geom.H * c.a.gq % 4 == 0 && c.n_records <= 4)   // (four rows of a wave are one token's)
+  if (rows >= MERGE_ROWS_MANY && c.a.geom.H * c.a.gq % 4 == 0 && c.usual_records <= 4)   // (four rows of a wave are one token's)
     hipLaunchKernelGGL((page_merge_shared_kernel<4, 4>), dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, st, c, bf ? 1 : 0);
-  else if (c.n_records <= 8) hipLaunchKernelGGL((page_merge_shared_kernel<1, 8>), blocks, dim3(256), 0, st, c, bf ? 1 : 0);
+  else if (c.usual_records <= 8) hipLaunchKernelGGL((page_merge_shared_kernel<1, 8>), blocks, dim3(256), 0, st, c, bf ? 1 : 0);
   else hipLaunchKernelGGL((page_merge_shared_kernel<1, 16>), blocks, dim3(256), 0, st, c, bf ? 1 : 0);
   return hipGetLastError();
 }

@@ -39,6 +39,20 @@ static Parted prefix_parts(double blocks, double filled, int most, int keys, int
   return best;
 }
 
+// What a sequence has behind its prefix is longer than `own` tokens, max_kv less the longest prefix, where it is in no group or in one with a shorter prefix: then it may be all of max_kv,
+// which only the device knows.  So parts have a length, that of `own` in k.n_split parts or, where `own` is one part, what takes (at ns_per_key) half as long as the call by itself; and there are as
+// many as max_kv has.  Most sequences have one: blocks of parts that are not there leave at once, 1000 of them in 1.6 us, and are no more than eight rounds.
+// Of one length up to max_kv (one part, whatever was there) 16 sequences behind 16000 tokens and one of 16000 by itself took 200 us and take 67, gear_page_attn 121; 8 behind 32000 and 8 of
+// 31000 behind 500 686, 229 and 241; 6 behind 32000 and two by themselves 578, 117 and 127; 4 of 7300 behind 1000 and 4 behind 8192 104, 41 and 43.
+// Longest parts of a third of the call: 250 in the second, 41.2 instead of 39.7 where nobody has more than `own` (48 sequences of five groups behind up to 6001).
+constexpr int LONGER_LEAST = 1024;
+static void divide_longer(SharedKind& k, int own, int max_kv, int64_t blocks, int64_t rows, double by_itself, double ns_per_key) {
+  const int parts = k.n_split;
+  k.least = parts > 1 ? own / parts : std::max(std::max(own, LONGER_LEAST), (int)std::min(0.5 * by_itself / ns_per_key, (double)max_kv));
+  const int64_t wanted = ((int64_t)max_kv + k.least / 2) / k.least, most = std::min(DIVIDED_MOST / rows, 8 * (int64_t)MANY_SLOTS / std::max(blocks, (int64_t)1));
+  k.n_split = (int)std::max((int64_t)parts, std::min(wanted, most));
+}
+
 static SharedPlan shared_plan(int H, int gq, const gear_page_batch& b, const gear_page_groups& gr, int bytes_per_key) {
   SharedPlan p{};
   const int64_t rows = (int64_t)b.n_tokens * H * gq, all_cols = (int64_t)b.n_tokens * gq;
@@ -51,12 +65,20 @@ static SharedPlan shared_plan(int H, int gq, const gear_page_batch& b, const gea
   const int few_limit = !few ? 0 : all_few ? (int)seq_cols : gq <= 16 ? 16 : FEW_COLS_MOST;
   p.tiles = few_limit <= 16 && (!prefix_few || group_cols <= 16) ? 1 : 2;
   const double record_bytes = (double)rows * RECORD_BYTES, codes = bytes_per_key < 4 * D ? 1.3 : 1.0;
+  // gear_page_attn's time, whose repeated reads of the shared pages the caches serve: 0.04 ns per sequence, KV head and key with few columns (64 sequences of 8300 to 9200 tokens, 8 heads,
+  // 174 us, 16 of 2100, 32 heads, 44), 2.36 us per tile of 128 columns and 64 keys on 512 places with many (16 of 6150, 20 to 60 new tokens, 32 query heads over 8: 125 us, shared 97).
+  const double filled = gr.n_groups >= 4 ? 0.65 : 1.0, keys = (prefix * filled + 0.6 * own) * (double)b.n_seqs * H;
+  const double by_itself = all_few ? 7000.0 + 0.04 * (few_limit <= 16 ? 1.0 : 1.4) * keys
+                                   : 8000.0 + keys / MANY_KEYS * std::ceil((double)all_cols / b.n_seqs / MANY_COLS) * 2360.0 * codes / MANY_SLOTS;
   // parts of what lies behind the prefixes
   p.own_few = SharedKind{1, FEW_PART, few_limit, 0, 0};
   p.own_many = SharedKind{1, MANY_PART, few_limit, (int)(all_cols / MANY_COLS + b.n_seqs), 0};
+  int usual = 1;   // parts of `own` tokens
   if (few) {
     p.own_few.n_split = best_parts((int64_t)b.n_seqs * H, 1.0, FEW_SLOTS, FEW_BLOCKS_MOST, own, FEW_PART, 4000.0, FEW_PART / 2, 1.0, 0.0, record_bytes, 0.0);
     while (p.own_few.n_split > 1 && rows * p.own_few.n_split > DIVIDED_MOST) --p.own_few.n_split;
+    usual = p.own_few.n_split;
+    divide_longer(p.own_few, own, b.max_kv, (int64_t)b.n_seqs * H, rows, by_itself, 2000.0 / (FEW_PART / 2));
   }
   // ... and of the prefixes, for each tile of columns
   const int64_t tiles = prefix_few ? gr.n_groups : std::max((all_cols + MANY_COLS - 1) / MANY_COLS, (int64_t)gr.n_groups);
@@ -65,7 +87,7 @@ static SharedPlan shared_plan(int H, int gq, const gear_page_batch& b, const gea
   const int least = prefix_few ? FEW_PART : MANY_PART;
   const int64_t by_blocks = MANY_BLOCKS_MOST / std::max(tiles * H, (int64_t)1), by_records = std::max(DIVIDED_MOST / rows, (int64_t)1);
   const int most = (int)std::max((int64_t)1, std::min((int64_t)(prefix / least), std::min(by_blocks, by_records)));
-  const double filled = gr.n_groups >= 4 ? 0.65 : 1.0, own_ns = 6000.0 + 0.6 * (double)b.n_seqs * H * own * bytes_per_key / 4.5e3;
+  const double own_ns = 6000.0 + 0.6 * (double)b.n_seqs * H * own * bytes_per_key / 4.5e3;
   const Parted parts = prefix_few ? prefix_parts((double)(tiles * H), filled, most, prefix, FEW_PART / 2, 2000.0, 2500.0, own_ns, record_bytes)
                                   : prefix_parts((double)(tiles * H), filled, most, prefix, MANY_KEYS, 1500.0 * codes, 2360.0 * codes, own_ns, record_bytes);
   p.prefix.n_split = parts.n;
@@ -74,12 +96,8 @@ static SharedPlan shared_plan(int H, int gq, const gear_page_batch& b, const gea
   p.own_many.blocks = many ? 1 : 0;
   const int n_own = std::max(p.own_few.n_split, p.own_many.n_split);
   p.records = rows * (p.prefix.n_split + n_own);
-  // Against gear_page_attn, whose repeated reads of the shared pages the caches serve: 0.04 ns per sequence, KV head and key with few columns (64 sequences of 8300 to 9200 tokens, 8 heads,
-  // 174 us, 16 of 2100, 32 heads, 44), 2.36 us per tile of 128 columns and 64 keys on 512 places with many (16 of 6150, 20 to 60 new tokens, 32 query heads over 8: 125 us, shared 97).
-  const double shared = parts.time + 4000.0 + record_bytes * n_own * 2.0 / 5000.0;
-  const double keys = (prefix * filled + 0.6 * own) * (double)b.n_seqs * H;
-  const double by_itself = all_few ? 7000.0 + 0.04 * (p.own_few.few <= 16 ? 1.0 : 1.4) * keys
-                                   : 8000.0 + keys / MANY_KEYS * std::ceil((double)all_cols / b.n_seqs / MANY_COLS) * 2360.0 * codes / MANY_SLOTS;
+  p.usual_records = p.prefix.n_split + usual;
+  const double shared = parts.time + 4000.0 + record_bytes * usual * 2.0 / 5000.0;
   p.shared = gr.always != 0 || shared < by_itself;
   return p;
 }
@@ -133,6 +151,7 @@ int gear_page_attn_shared(const gear_page_config* cfg, const void* pool, size_t 
   c.own_few = p.own_few;
   c.own_many = p.own_many;
   c.n_records = p.prefix.n_split + std::max(p.own_few.n_split, p.own_many.n_split);
+  c.usual_records = p.usual_records;
   const int64_t prefix_blocks = (int64_t)H * p.prefix.n_split * (p.prefix.few > 0 ? gr.n_groups : p.prefix.tiles);
   const int64_t few_blocks = (int64_t)H * p.own_few.n_split * b.n_seqs * p.own_few.blocks, many_blocks = (int64_t)H * p.own_many.n_split * p.own_many.tiles * p.own_many.blocks;
   if (prefix_blocks + few_blocks + many_blocks > THREADS_MOST / 512 || (int64_t)b.n_tokens * H_q > THREADS_MOST / 256) return GEAR_ECAPACITY;
