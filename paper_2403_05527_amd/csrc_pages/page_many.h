@@ -151,8 +151,10 @@ __device__ __forceinline__ void many_columns(const Attn& a, int bid, unsigned ch
   const PageGeom& g = a.geom;
   const int lane = lane_id(), wave = GEAR_WAVE_UNIFORM((int)(threadIdx.x >> 6)), c = lane & 31, half = lane >> 5;
   // heads next to each other: with 8 of them and more, a head's tiles share one XCD's L2
-  const int head = bid % g.H, rest = bid / g.H, part = rest % a.n_split;
-  const ColTile ct = col_tile(a, rest / a.n_split, lane);
+  const int head = bid % g.H;
+  const Place place = many_place(a, bid / g.H);
+  const int part = place.part;
+  const ColTile ct = col_tile(a, place.i, lane);
   if (ct.s < 0) return;
   const int s = ct.s, col0 = ct.col0;
   const Span span = span_of(a, s);

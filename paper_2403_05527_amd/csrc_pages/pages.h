@@ -253,11 +253,12 @@ struct Span {
   int begin;       // the first key of the block's parts, a multiple of MANY_KEYS
   int table_row;
 };
-// The blocks of a head in their order: sequences (of few columns), each in n_split parts.
+// The blocks of a head in their order: sequences (of few columns) or column tiles (of many), each in n_split parts.
 struct Place {
   int i, part;
 };
 __device__ __forceinline__ Place few_place(const PageAttn& a, int at) { return Place{at / a.n_split, at % a.n_split}; }
+__device__ __forceinline__ Place many_place(const PageAttn& a, int at) { return Place{at / a.n_split, at % a.n_split}; }
 __device__ __forceinline__ Span span_of(const PageAttn& a, int s) { return Span{seq_span(a, s), 0, s}; }
 // whether the one part that a row has is its output, and where a part's record lies
 __device__ __forceinline__ bool is_output(const PageAttn&, const Span&, int parts) { return parts == 1; }

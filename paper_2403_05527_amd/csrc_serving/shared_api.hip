@@ -45,6 +45,8 @@ static Parted prefix_parts(double blocks, double filled, int most, int keys, int
 // Of one length up to max_kv (one part, whatever was there) 16 sequences behind 16000 tokens and one of 16000 by itself took 200 us and take 67, gear_page_attn 121; 8 behind 32000 and 8 of
 // 31000 behind 500 686, 229 and 241; 6 behind 32000 and two by themselves 578, 117 and 127; 4 of 7300 behind 1000 and 4 behind 8192 104, 41 and 43.
 // Longest parts of a third of the call: 250 in the second, 41.2 instead of 39.7 where nobody has more than `own` (48 sequences of five groups behind up to 6001).
+// Of many columns (undivided, now, gear_page_attn): two chunks of 64 tokens with 50000 behind 1000 1420, 173 and 180 us; a chunk of 512 with 30000 beside 15 single tokens 908, 575 and 620;
+// 16 questions about 6100 tokens of which one has 30000 more 582, 325 and 407.  With parts of two thirds of these, questions that have no more than 60 tokens 81.7 instead of 79.8.
 constexpr int LONGER_LEAST = 1024;
 static void divide_longer(SharedKind& k, int own, int max_kv, int64_t blocks, int64_t rows, double by_itself, double ns_per_key) {
   const int parts = k.n_split;
@@ -77,8 +79,16 @@ static SharedPlan shared_plan(int H, int gq, const gear_page_batch& b, const gea
   if (few) {
     p.own_few.n_split = best_parts((int64_t)b.n_seqs * H, 1.0, FEW_SLOTS, FEW_BLOCKS_MOST, own, FEW_PART, 4000.0, FEW_PART / 2, 1.0, 0.0, record_bytes, 0.0);
     while (p.own_few.n_split > 1 && rows * p.own_few.n_split > DIVIDED_MOST) --p.own_few.n_split;
-    usual = p.own_few.n_split;
+    usual = std::max(usual, p.own_few.n_split);
     divide_longer(p.own_few, own, b.max_kv, (int64_t)b.n_seqs * H, rows, by_itself, 2000.0 / (FEW_PART / 2));
+  }
+  if (many) {
+    const int64_t blocks = (all_cols + MANY_COLS - 1) / MANY_COLS * H;
+    p.own_many.n_split = best_parts(blocks, 1.0, MANY_SLOTS, MANY_BLOCKS_MOST, own, LONGER_LEAST, 6000.0, MANY_KEYS, 1.0, 0.0, record_bytes, 0.0);
+    const int64_t places = (int64_t)p.own_many.tiles * H;
+    while (p.own_many.n_split > 1 && (rows * p.own_many.n_split > DIVIDED_MOST || places * p.own_many.n_split > 8 * MANY_SLOTS)) --p.own_many.n_split;
+    usual = std::max(usual, p.own_many.n_split);
+    divide_longer(p.own_many, own, b.max_kv, places, rows, by_itself, 1500.0 * codes / MANY_KEYS);
   }
   // ... and of the prefixes, for each tile of columns
   const int64_t tiles = prefix_few ? gr.n_groups : std::max((all_cols + MANY_COLS - 1) / MANY_COLS, (int64_t)gr.n_groups);

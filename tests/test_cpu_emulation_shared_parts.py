@@ -13,6 +13,9 @@ LONGER = {
     "a_short_prefix": (BF16, 8, 64, 32, 1, 4, [(3000, [(1, 5)] * 2), (70, [(1, 3050), (1, 20)])], 0, 1, 1),
     "two_column_tiles": (F16, 4, 32, 16, 1, 4, [(2600, [(5, 6)] * 2), (0, [(6, 2700), (5, 30)])], 1, 0, 0),
     "prefixes_of_many_columns": (F16, 16, 128, 64, 1, 4, [(1900, [(1, 5)] * 9), (0, [(1, 2000)])], 1, 1, 2),
+    "many_behind": (F16, 16, 128, 16, 1, 4, [(64, [(9, 12), (33, 1700), (9, 9)]), (1500, [(1, 300), (2, 5)])], 0, 1, 1),
+    "many_by_itself": (BF16, 4, 64, 16, 1, 2, [(1800, [(17, 30)] * 2), (0, [(80, 2000), (1, 1950)])], 1, 1, 0),
+    "many_see_all": (F16, 8, 64, 64, 1, 4, [(1800, [(9, 30)] * 2), (0, [(33, 1900)])], 1, 0, 0),
     "no_page": (F16, 16, 128, 16, 1, 2, [(2500, [(1, 5), (1, 9)]), (0, [(1, 2600), (0, 40)])], 1, 1, 0),
 }
 

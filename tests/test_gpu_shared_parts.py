@@ -13,6 +13,10 @@ LONGER = [
     (16, 1, 8, [(3000, [(1, 9)] * 20), (0, [(1, 3000 - 700 * i) for i in range(4)])], 1, 2),                 # prefixes of many columns
     (16, 2, 4, [(2600, [(5, 20)] * 2), (0, [(5, 2600), (2, 10)])], 1, 0),                                    # two tiles of columns
     (128, 1, 2, [(2500, [(1, 1 + i % 7)] * 2) for i in range(30)] + [(0, [(1, 2500 - i) for i in range(9)])], 1, 0),   # more sequences than a wave has lanes
+    (16, 2, 4, [(64, [(9, 12), (70, 3500), (9, 9)]), (2900, [(1, 300), (2, 5)])], 0, 1),                      # many columns, behind a short prefix
+    (64, 1, 8, [(3000, [(5, 30)] * 9), (0, [(100, 3300), (1, 3200), (40, 60)])], 1, 0),                        # by themselves
+    (16, 1, 2, [(2000, [(1, 1 + i % 7)] * 2) for i in range(30)] + [(0, [(70, 2100), (1, 1900), (33, 2222)])], 1, 0),
+    (32, 2, 3, [(128, [(50, 5000), (43, 4100)])], 0, 3),                                                     # all of them long
     (256, 1, 1, [(70, [(1, 5)] * 2), (12000, [(0, 3), (1, 7)]), (0, [(1, 12000), (0, 5)])], 1, 0),
 ]
 

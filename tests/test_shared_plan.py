@@ -59,14 +59,14 @@ def behind(groups):
 
 
 def longest(plan, gq, groups):
-    """The longest block behind the prefixes in us: 2 us per 128 keys with few columns, 2.36 per 64 with many (what the kernels' blocks took)."""
+    """The longest block behind the prefixes in us: 2 us per 128 keys with few columns, 1.5 per 64 with many (what the kernels' blocks take that have a CU to themselves)."""
     few, many = plan["few"], plan["many"]
     most = 0.0
     for n, keys in behind(groups):
         if few["few"] and n <= few["few"] and n * gq <= few["few"]:
             most = max(most, 2.0 * -(-part_length(keys, few, 32) // 128))
         else:
-            most = max(most, 2.36 * -(-part_length(keys, many, 64) // 64))
+            most = max(most, 1.5 * -(-part_length(keys, many, 64) // 64))
     return most
 
 
@@ -81,11 +81,17 @@ FEW = {
     "a few tokens each": (sequences((4000, [(5, 200)] * 12), (None, [(5, 4000)] * 4)), 47),
 }
 
+MANY = {
+    "two chunks": (sequences((1000, [(64, 50000)] * 2)), 180),
+    "a chunk beside single tokens": (sequences((2000, [(512, 30000)] + [(1, 30000)] * 15)), 620),
+    "a long question": (sequences((6100, [(40, 60)] * 15 + [(40, 30000)])), 407),
+}
 
-@pytest.mark.parametrize("name", list(FEW))
+
+@pytest.mark.parametrize("name", list(FEW) + list(MANY))
 def test_what_lies_behind_is_divided_by_its_own_length(planner, name):
     """No block behind the prefixes takes longer than gear_page_attn for the whole batch, whichever sequence the longest is."""
-    groups, plain = FEW[name]
+    groups, plain = FEW.get(name) or MANY[name]
     (kind, plan), = plans(planner, [call(8, 4, 16, groups)])
     assert kind == "shared"
     assert longest(plan, 4, groups) <= plain, plan
@@ -94,17 +100,20 @@ def test_what_lies_behind_is_divided_by_its_own_length(planner, name):
 def test_usual_batches_keep_their_parts(planner):
     """Where nobody has more behind the prefix than the longest sequence has behind the longest prefix, one part each, as blocks that begin at once."""
     usual = [(32, 1, 16, sequences((2077, [(1, 64)] * 16))), (8, 4, 16, sequences((8192, [(1, 1000)] * 64))), (8, 4, 8, sequences(*[(p, [(1, 700)] * 10) for p in (1500, 6001, 3000, 5200, 2222)]))]
+    usual += [(8, 4, 16, sequences((6100, [(n, n) for n in range(20, 60, 3)])))]
     for H, gq, bits, groups in usual:
         (kind, plan), = plans(planner, [call(H, gq, bits, groups)])
-        assert kind == "shared" and all(part_length(keys, plan["few"], 32) >= keys for _, keys in behind(groups))
+        which, unit = ("few", 32) if all(n * gq <= 32 for n, _ in behind(groups)) else ("many", 64)
+        assert kind == "shared" and all(part_length(keys, plan[which], unit) >= keys for _, keys in behind(groups))
 
 
 def test_blocks_and_records_stay_bounded(planner):
     calls = [(H, gq, 16, seqs, seqs * q, q, kv, 1, seqs * q, prefix, 1)
              for H, gq in ((1, 1), (8, 4), (32, 1), (8, 8)) for seqs in (1, 3, 64, 900, 30000) for q in (1, 4, 40, 700) for kv in (1, 1500, 40000, 2 ** 30) for prefix in (64, 1000, 39000) if seqs * q < 50000]
+    calls += [(8, 4, 16, 400000, 40, 40, 40000, 1, 40, prefix, 1) for prefix in (64, 39000)]                # all but a few without new tokens
     for c, (kind, plan) in zip(calls, plans(planner, calls)):
         H, gq, _, seqs, tokens = c[:5]
         assert kind in ("shared", "plain")
         if plan:
             rows = tokens * H * gq
-            assert rows * plan["records"] <= 2 * max(rows, 768 * 128) and plan["few"]["blocks"] <= max(seqs * H, 4096), (c, plan)
+            assert rows * plan["records"] <= 2 * max(rows, 768 * 128) and plan["few"]["blocks"] <= max(seqs * H, 4096) and plan["many"]["blocks"] <= max((tokens * gq // 128 + seqs) * H, 4096), (c, plan)
