@@ -97,7 +97,15 @@ static SharedPlan shared_plan(int H, int gq, const gear_page_batch& b, const gea
   const int least = prefix_few ? FEW_PART : MANY_PART;
   const int64_t by_blocks = MANY_BLOCKS_MOST / std::max(tiles * H, (int64_t)1), by_records = std::max(DIVIDED_MOST / rows, (int64_t)1);
   const int most = (int)std::max((int64_t)1, std::min((int64_t)(prefix / least), std::min(by_blocks, by_records)));
-  const double own_ns = 6000.0 + 0.6 * (double)b.n_seqs * H * own * bytes_per_key / 4.5e3;
+  // As far as the bounds show that there are sequences in no group, those have up to max_kv tokens: their bytes, and the longest part of one, which the chip waits for.  (14 questions about
+  // 6100 tokens and two by themselves: 147 us shared, 105 as gear_page_attn.  Fewer parts of the prefix beside what lies behind: 6 sequences behind 32000 and two by themselves 118 -> 99 us, 24 of 8 bits behind
+  // 6001 and 8 53 -> 42.)
+  const int64_t covered = (int64_t)gr.n_groups * gr.max_q;
+  const double outside = covered < b.n_tokens ? (double)(b.n_tokens - covered) * b.n_seqs / b.n_tokens : 0.0;   // sequences
+  double own_ns = 6000.0 + 0.6 * ((b.n_seqs - outside) * own + outside * b.max_kv) * H * bytes_per_key / 4.5e3;
+  const int longest = std::min(b.max_kv, 1 << 29);   // (sums within 32 bits)
+  if (outside > 0.0 && few) own_ns = std::max(own_ns, 4000.0 + 2000.0 / (FEW_PART / 2) * parts_of(longest, p.own_few.n_split, p.own_few.least, KEY_STEP).len);
+  if (outside > 0.0 && many) own_ns = std::max(own_ns, 6000.0 + 1500.0 * codes / MANY_KEYS * parts_of(longest, p.own_many.n_split, p.own_many.least, MANY_KEYS).len);
   const Parted parts = prefix_few ? prefix_parts((double)(tiles * H), filled, most, prefix, FEW_PART / 2, 2000.0, 2500.0, own_ns, record_bytes)
                                   : prefix_parts((double)(tiles * H), filled, most, prefix, MANY_KEYS, 1500.0 * codes, 2360.0 * codes, own_ns, record_bytes);
   p.prefix.n_split = parts.n;

@@ -97,6 +97,28 @@ def test_what_lies_behind_is_divided_by_its_own_length(planner, name):
     assert longest(plan, 4, groups) <= plain, plan
 
 
+# batches, and us shared and not
+CHOICE = {
+    "samples": (32, 1, 16, sequences((2077, [(1, 64)] * 16)), 18, 47),
+    "a system prompt": (8, 4, 16, sequences((8192, [(1, 550)] * 64)), 48, 165),
+    "unequal groups": (8, 4, 8, sequences(*[(p, [(1, 700)] * 10) for p in (1500, 6001, 3000, 5200, 2222)]), 39, 83),
+    "questions": (8, 4, 16, sequences((6100, [(n, n) for n in range(20, 61, 3)])), 90, 127),
+    "one by itself": (8, 4, 16, sequences((16000, [(1, 20)] * 16), (None, [(1, 16000)])), 62, 120),
+    "two by themselves": (8, 4, 16, sequences((32000, [(1, 100)] * 6), (None, [(1, 32000)] * 2)), 99, 127),
+    "one of 64 by itself": (8, 4, 16, sequences((8192, [(1, 550)] * 63), (None, [(1, 9000)])), 88, 168),
+    "eight of 32 by themselves": (8, 4, 8, sequences((6001, [(1, 400)] * 24), (None, [(1, 6000)] * 8)), 42, 53),
+    "questions by themselves": (8, 4, 16, sequences((6100, [(40, 60)] * 14), (None, [(40, 6000)] * 2)), 147, 105),
+    "a question by itself": (8, 4, 16, sequences((6100, [(40, 900)] * 15), (None, [(40, 6500)])), 155, 112),
+}
+
+
+@pytest.mark.parametrize("name", list(CHOICE))
+def test_prefixes_are_shared_where_that_is_faster(planner, name):
+    H, gq, bits, groups, shared, plain = CHOICE[name]
+    (kind, _), = plans(planner, [call(H, gq, bits, groups, always=0)])
+    assert kind == ("shared" if shared < plain else "plain")
+
+
 def test_usual_batches_keep_their_parts(planner):
     """Where nobody has more behind the prefix than the longest sequence has behind the longest prefix, one part each, as blocks that begin at once."""
     usual = [(32, 1, 16, sequences((2077, [(1, 64)] * 16))), (8, 4, 16, sequences((8192, [(1, 1000)] * 64))), (8, 4, 8, sequences(*[(p, [(1, 700)] * 10) for p in (1500, 6001, 3000, 5200, 2222)]))]
