@@ -117,11 +117,11 @@ __device__ __forceinline__ int few_sequence(const SharedPart& a, int i) {
   return GEAR_WAVE_UNIFORM(__ffsll((long long)__ballot(lane < a.n_seqs && before == i)) - 1);
 }
 
-// Of what lies behind the prefixes all first parts come first: few sequences have more, and the blocks of parts that are not there leave at the end.
+// Of what lies behind the prefixes all first parts come first: few sequences have more, and the blocks of parts that are not there leave at the end, without looking for the longest.
 __device__ __forceinline__ Place few_place(const SharedPart& a, int at) {
   if (a.prefix) return few_place(static_cast<const PageAttn&>(a), at);
-  const int part = a.n_split == 1 ? 0 : at / a.n_seqs;
-  return Place{few_sequence(a, at - part * a.n_seqs), part};
+  const int part = a.n_split == 1 ? 0 : at / a.n_seqs, i = at - part * a.n_seqs;
+  return Place{part == 0 ? few_sequence(a, i) : i, part};
 }
 __device__ __forceinline__ Place many_place(const SharedPart& a, int at) {
   if (a.prefix) return many_place(static_cast<const PageAttn&>(a), at);

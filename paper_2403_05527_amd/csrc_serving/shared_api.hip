@@ -40,18 +40,18 @@ static Parted prefix_parts(double blocks, double filled, int most, int keys, int
 }
 
 // What a sequence has behind its prefix is longer than `own` tokens, max_kv less the longest prefix, where it is in no group or in one with a shorter prefix: then it may be all of max_kv,
-// which only the device knows.  So parts have a length, that of `own` in k.n_split parts or, where `own` is one part, what takes (at ns_per_key) half as long as the call by itself; and there are as
-// many as max_kv has.  Most sequences have one: blocks of parts that are not there leave at once, 1000 of them in 1.6 us, and are no more than eight rounds.
-// Of one length up to max_kv (one part, whatever was there) 16 sequences behind 16000 tokens and one of 16000 by itself took 200 us and take 67, gear_page_attn 121; 8 behind 32000 and 8 of
-// 31000 behind 500 686, 229 and 241; 6 behind 32000 and two by themselves 578, 117 and 127; 4 of 7300 behind 1000 and 4 behind 8192 104, 41 and 43.
-// Longest parts of a third of the call: 250 in the second, 41.2 instead of 39.7 where nobody has more than `own` (48 sequences of five groups behind up to 6001).
-// Of many columns (undivided, now, gear_page_attn): two chunks of 64 tokens with 50000 behind 1000 1420, 173 and 180 us; a chunk of 512 with 30000 beside 15 single tokens 908, 575 and 620;
-// 16 questions about 6100 tokens of which one has 30000 more 582, 325 and 407.  With parts of two thirds of these, questions that have no more than 60 tokens 81.7 instead of 79.8.
+// which only the device knows.  So parts have a length, and there are as many as bring the longest to half of what the call takes by itself (at ns_per_key), in as many blocks as the chip holds
+// twice: most sequences have no more than the usual, and blocks of parts that are not there leave at once, 1000 of them in 2 to 6 us.
+// In one part, whatever was there, 16 sequences behind 16000 tokens and one of 16000 by itself took 200 us and take 61, gear_page_attn 120; 8 behind 32000 and 8 of
+// 31000 behind 500 686, 227 and 240; 6 behind 32000 and two by themselves 578, 99 and 127; 4 of 7300 behind 1000 and 4 behind 8192 104, 41 and 42.
+// Of many columns: two chunks of 64 tokens with 50000 behind 1000 1420, 167 and 160 to 180 us; a chunk of 512 with 30000 beside 15 single tokens 908, 548 and 607;
+// 16 questions about 6100 tokens of which one has 30000 more 582, 310 and 405.  With parts of two thirds of these, questions that have no more than 60 tokens 81.7 instead of 79.8.
+// (In blocks for eight times what the chip holds: 58 sequences of 7 heads behind 4060 tokens, of which none has more, 36 us instead of 31.)
 constexpr int LONGER_LEAST = 1024;
 static void divide_longer(SharedKind& k, int own, int max_kv, int64_t blocks, int64_t rows, double by_itself, double ns_per_key) {
-  const int parts = k.n_split;
-  k.least = parts > 1 ? own / parts : std::max(std::max(own, LONGER_LEAST), (int)std::min(0.5 * by_itself / ns_per_key, (double)max_kv));
-  const int64_t wanted = ((int64_t)max_kv + k.least / 2) / k.least, most = std::min(DIVIDED_MOST / rows, 8 * (int64_t)MANY_SLOTS / std::max(blocks, (int64_t)1));
+  const int parts = k.n_split, enough = std::max(std::max(own / parts, LONGER_LEAST), (int)std::min(0.5 * by_itself / ns_per_key, (double)max_kv));
+  k.least = parts > 1 ? own / parts : enough;
+  const int64_t wanted = ((int64_t)max_kv + enough / 2) / enough, most = std::min(DIVIDED_MOST / rows, 2 * (int64_t)MANY_SLOTS / std::max(blocks, (int64_t)1));
   k.n_split = (int)std::max((int64_t)parts, std::min(wanted, most));
 }
 

@@ -138,4 +138,4 @@ def test_blocks_and_records_stay_bounded(planner):
         assert kind in ("shared", "plain")
         if plan:
             rows = tokens * H * gq
-            assert rows * plan["records"] <= 2 * max(rows, 768 * 128) and plan["few"]["blocks"] <= max(seqs * H, 4096) and plan["many"]["blocks"] <= max((tokens * gq // 128 + seqs) * H, 4096), (c, plan)
+            assert rows * plan["records"] <= 2 * max(rows, 768 * 128) and plan["few"]["blocks"] <= max(seqs * H, 1024) and plan["many"]["blocks"] <= max((tokens * gq // 128 + seqs) * H, 4096), (c, plan)
