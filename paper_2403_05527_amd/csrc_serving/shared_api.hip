@@ -15,26 +15,32 @@ static int64_t records_bound(int64_t rows, int max_kv, int max_prefix) {
 }
 
 // Estimates of a call's time, in ns; they choose the parts of the prefixes, and whether they are shared at all.
-struct Parted {
-  int n;
-  double time;
+// Of prefixes in equal parts, `real` blocks in all: a part takes 8 us and, per `step` keys, `alone`, or `beside` where two blocks share a CU.  What lies behind takes `own` by itself, and runs on the
+// places that the prefixes' blocks leave until they have ended; the records (`records` bytes) are written and read at 5 TB/s.
+struct Shared {
+  double prefix;   // until the prefixes' blocks have ended
+  double left;     // of the places, for others meanwhile
+  double all;
 };
-// The number of equal parts of the prefixes that is the fastest: `blocks` of them undivided, of which `filled` have keys; a part takes 8 us and, per `step` keys, `alone`, or
-// `beside` where two blocks share a CU.  What lies behind takes `own` by itself, and runs on the places that the prefixes' blocks leave until they have ended; the records (`records` bytes per
-// part) are written and read at 5 TB/s.  Where much lies behind, the prefixes' blocks are no more than the CUs.
+static Shared shared_time(double real, int n, int keys, int step, double alone, double beside, double own, double records) {
+  const double steps = (double)((((int64_t)keys + n - 1) / n + step - 1) / step), left = real < MANY_SLOTS ? 1.0 - real / MANY_SLOTS : 0.0;
+  double block = steps * beside;
+  if (real <= GEAR_PAGE_CUS && block > own / left) block = own / left + (steps - own / left / beside) * alone;
+  const double prefix = std::ceil(real / MANY_SLOTS) * (8000.0 + block), rest = own - prefix * left;
+  return Shared{prefix, left, prefix + (rest > 0.0 ? rest : 0.0) + records * 2.0 / 5000.0};
+}
+// The number of parts that is the fastest, of `blocks` undivided ones, of which `filled` have keys.  Where much lies behind, the prefixes' blocks are no more than the CUs.
 // 64 sequences behind 8192 tokens, bf16, 8 KV heads, 100 to 1000 tokens of their own (37 us by themselves): 76, 50, 47, 54, 52 and 62 us in 4, 8, 12, 16, 24 and 32 parts, and 6 to 12
 // of joining; five groups of 1500 to 6001 tokens at 8 bits 47, 32, 34, 37 and 40 in 4, 8, 10, 12 and 24.  Prefixes alone, in 4, 8, 16 and 32 parts: 1024 tokens 13, 11, 11 and 14 us,
 // 16384 111, 62, 38 and 31.
-static Parted prefix_parts(double blocks, double filled, int most, int keys, int step, double alone, double beside, double own, double records) {
-  Parted best{1, 0.0};
+static int prefix_parts(double blocks, double filled, int most, int keys, int step, double alone, double beside, double own, double records) {
+  int best = 1;
+  double least = 0.0;
   for (int n = 1; n <= most; ++n) {
-    const double real = blocks * filled * n, steps = (double)((((int64_t)keys + n - 1) / n + step - 1) / step);
+    const double real = blocks * filled * n;
     if (n > 1 && own > 10000.0 && real > GEAR_PAGE_CUS) break;
-    const double left = real < MANY_SLOTS ? 1.0 - real / MANY_SLOTS : 0.0;   // of the places
-    double block = steps * beside;
-    if (real <= GEAR_PAGE_CUS && block > own / left) block = own / left + (steps - own / left / beside) * alone;
-    const double prefix = std::ceil(real / MANY_SLOTS) * (8000.0 + block), rest = own - prefix * left, t = prefix + (rest > 0.0 ? rest : 0.0) + records * n * 2.0 / 5000.0;
-    if (n == 1 || t < best.time) best = Parted{n, t};
+    const double t = shared_time(real, n, keys, step, alone, beside, own, records * n).all;
+    if (n == 1 || t < least) best = n, least = t;
   }
   return best;
 }
@@ -69,7 +75,7 @@ static SharedPlan shared_plan(int H, int gq, const gear_page_batch& b, const gea
   const double record_bytes = (double)rows * RECORD_BYTES, codes = bytes_per_key < 4 * D ? 1.3 : 1.0;
   // gear_page_attn's time, whose repeated reads of the shared pages the caches serve: 0.04 ns per sequence, KV head and key with few columns (64 sequences of 8300 to 9200 tokens, 8 heads,
   // 174 us, 16 of 2100, 32 heads, 44), 2.36 us per tile of 128 columns and 64 keys on 512 places with many (16 of 6150, 20 to 60 new tokens, 32 query heads over 8: 125 us, shared 97).
-  const double filled = gr.n_groups >= 4 ? 0.65 : 1.0, keys = (prefix * filled + 0.6 * own) * (double)b.n_seqs * H;
+  const double keys = (prefix + 0.6 * own) * (double)b.n_seqs * H;
   const double by_itself = all_few ? 7000.0 + 0.04 * (few_limit <= 16 ? 1.0 : 1.4) * keys
                                    : 8000.0 + keys / MANY_KEYS * std::ceil((double)all_cols / b.n_seqs / MANY_COLS) * 2360.0 * codes / MANY_SLOTS;
   // parts of what lies behind the prefixes
@@ -102,20 +108,24 @@ static SharedPlan shared_plan(int H, int gq, const gear_page_batch& b, const gea
   // 6001 and 8 53 -> 42.)
   const int64_t covered = (int64_t)gr.n_groups * gr.max_q;
   const double outside = covered < b.n_tokens ? (double)(b.n_tokens - covered) * b.n_seqs / b.n_tokens : 0.0;   // sequences
-  double own_ns = 6000.0 + 0.6 * ((b.n_seqs - outside) * own + outside * b.max_kv) * H * bytes_per_key / 4.5e3;
-  const int longest = std::min(b.max_kv, 1 << 29);   // (sums within 32 bits)
-  if (outside > 0.0 && few) own_ns = std::max(own_ns, 4000.0 + 2000.0 / (FEW_PART / 2) * parts_of(longest, p.own_few.n_split, p.own_few.least, KEY_STEP).len);
-  if (outside > 0.0 && many) own_ns = std::max(own_ns, 6000.0 + 1500.0 * codes / MANY_KEYS * parts_of(longest, p.own_many.n_split, p.own_many.least, MANY_KEYS).len);
-  const Parted parts = prefix_few ? prefix_parts((double)(tiles * H), filled, most, prefix, FEW_PART / 2, 2000.0, 2500.0, own_ns, record_bytes)
-                                  : prefix_parts((double)(tiles * H), filled, most, prefix, MANY_KEYS, 1500.0 * codes, 2360.0 * codes, own_ns, record_bytes);
-  p.prefix.n_split = parts.n;
-  p.prefix.least = std::max(prefix / parts.n, least);
+  const double own_ns = 6000.0 + 0.6 * ((b.n_seqs - outside) * own + outside * b.max_kv) * H * bytes_per_key / 4.5e3;
+  const int longest = outside > 0.0 ? std::min(b.max_kv, 1 << 29) : 0;   // (sums within 32 bits)
+  double part = 0.0;
+  if (longest > 0 && few) part = 4000.0 + 2000.0 / (FEW_PART / 2) * parts_of(longest, p.own_few.n_split, p.own_few.least, KEY_STEP).len;
+  if (longest > 0 && many) part = std::max(part, 6000.0 + 1500.0 * codes / MANY_KEYS * parts_of(longest, p.own_many.n_split, p.own_many.least, MANY_KEYS).len);
+  // (Where they are divided, prefixes are taken to be 0.65 of the longest in the mean from four groups on: five of 1500 to 6001 tokens 39 us, 47 taken to be 6001.  Not where the choice is made, by which
+  // 12 sequences behind 4096 tokens would be shared in three groups and not in four, 31.5 us for 23.7.)
+  const double blocks = (double)(tiles * H), alone = prefix_few ? 2000.0 : 1500.0 * codes, beside = prefix_few ? 2500.0 : 2360.0 * codes;
+  const int step = prefix_few ? FEW_PART / 2 : MANY_KEYS;
+  p.prefix.n_split = prefix_parts(blocks, gr.n_groups >= 4 ? 0.65 : 1.0, most, prefix, step, alone, beside, own_ns, record_bytes);
+  p.prefix.least = std::max(prefix / p.prefix.n_split, least);
   p.own_few.blocks = few ? 1 : 0;
   p.own_many.blocks = many ? 1 : 0;
   const int n_own = std::max(p.own_few.n_split, p.own_many.n_split);
   p.records = rows * (p.prefix.n_split + n_own);
   p.usual_records = p.prefix.n_split + usual;
-  const double shared = parts.time + 4000.0 + record_bytes * usual * 2.0 / 5000.0;
+  const Shared t = shared_time(blocks * (0.8 + 0.2 / gr.n_groups) * p.prefix.n_split, p.prefix.n_split, prefix, step, alone, beside, own_ns, record_bytes * p.prefix.n_split);
+  const double shared = std::max(t.all, (t.left > 0.1 ? 0.0 : t.prefix) + part) + 4000.0 + record_bytes * usual * 2.0 / 5000.0;
   p.shared = gr.always != 0 || shared < by_itself;
   return p;
 }

@@ -107,6 +107,11 @@ CHOICE = {
     "two by themselves": (8, 4, 16, sequences((32000, [(1, 100)] * 6), (None, [(1, 32000)] * 2)), 99, 127),
     "one of 64 by itself": (8, 4, 16, sequences((8192, [(1, 550)] * 63), (None, [(1, 9000)])), 88, 168),
     "eight of 32 by themselves": (8, 4, 8, sequences((6001, [(1, 400)] * 24), (None, [(1, 6000)] * 8)), 42, 53),
+    "three groups of one length": (8, 4, 16, sequences(*[(4096, [(1, 200)] * 4)] * 3), 22, 31),
+    "four": (8, 4, 16, sequences(*[(4096, [(1, 200)] * 3)] * 4), 24, 32),
+    "three of 24": (8, 4, 16, sequences(*[(2048, [(1, 200)] * 8)] * 3), 21, 28),
+    "four of 24": (8, 4, 16, sequences(*[(2048, [(1, 200)] * 6)] * 4), 22, 28),
+    "eight of 24": (8, 4, 16, sequences(*[(2048, [(1, 200)] * 3)] * 8), 24, 28),
     "questions by themselves": (8, 4, 16, sequences((6100, [(40, 60)] * 14), (None, [(40, 6000)] * 2)), 147, 105),
     "a question by itself": (8, 4, 16, sequences((6100, [(40, 900)] * 15), (None, [(40, 6500)])), 155, 112),
 }
