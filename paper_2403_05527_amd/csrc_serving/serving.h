@@ -41,6 +41,8 @@ constexpr int SLOT_THREADS = 256, SLOT_TOKENS = 1024;   // where the slots have 
 hipError_t launch_extend(const PageTable& t, const int32_t* rows, const int32_t* counts, int n, int most, int64_t* slots, int32_t* copies, int32_t* refused,
                          hipStream_t st);
 hipError_t launch_truncate(const PageTable& t, const int32_t* rows, const int32_t* lens, int n, hipStream_t st);
+constexpr int FORK_THREADS = 256, FORK_ENTRIES = 8192;   // entries of a block
+inline int fork_cols(int n) { return n > FORK_ENTRIES / 64 ? FORK_ENTRIES / n : 64; }   // columns of the table that a block has of n rows
 hipError_t launch_fork(const PageTable& t, const int32_t* src, const int32_t* dst, int n, hipStream_t st);
 hipError_t launch_compact(const PageTable& t, int32_t* moves, int most, int32_t* counts, hipStream_t st);
 constexpr int MOVE_THREADS = 256, MOVE_LOADS = 4, MOVE_BYTES = MOVE_THREADS * MOVE_LOADS * 16;   // a block's share of a page

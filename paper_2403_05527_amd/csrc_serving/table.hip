@@ -233,7 +233,6 @@ __global__ __launch_bounds__(DROP_THREADS) void page_truncate_kernel(PageTable t
 }
 
 // ---- rows copied: a block per FORK_ENTRIES / n columns of the table, all of whose sources it reads before it writes (5.3 us for 16 copies of 257 entries, latency)
-constexpr int FORK_THREADS = 256, FORK_ENTRIES = 8192;
 __global__ __launch_bounds__(FORK_THREADS) void page_fork_kernel(PageTable t, const int32_t* src, const int32_t* dst, int n, int cols) {
   GEAR_DYN_LDS(lds);
   int* from = reinterpret_cast<int*>(lds);          // [LIST_MOST] source row, -1: nothing to do
@@ -427,7 +426,7 @@ hipError_t launch_fork(const PageTable& t, const int32_t* src, const int32_t* ds
   static std::atomic<uint64_t> raised{0};
   const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(page_fork_kernel), raised, lds, LDS_PER_CU);
   if (e != hipSuccess) return e;
-  const int cols = std::min(64, FORK_ENTRIES / n);
+  const int cols = fork_cols(n);
   hipLaunchKernelGGL(page_fork_kernel, dim3((unsigned)((t.width + cols - 1) / cols)), dim3(FORK_THREADS), lds, st, t, src, dst, n, cols);
   return hipGetLastError();
 }

@@ -57,6 +57,7 @@ int gear_page_fork(const gear_page_table* t, const int32_t* src, const int32_t* 
   if (n > GEAR_PAGE_LIST_MAX) return GEAR_ECAPACITY;
   if (n == 0) return GEAR_OK;
   if ((rc = check_list(src, dst))) return rc;
+  if (((int64_t)p.width + fork_cols(n) - 1) / fork_cols(n) > THREADS_MOST / FORK_THREADS) return GEAR_ECAPACITY;
   return launch_fork(p, src, dst, n, static_cast<hipStream_t>(stream)) == hipSuccess ? GEAR_OK : GEAR_EHIP;
 }
 
