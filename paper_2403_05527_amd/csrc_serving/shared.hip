@@ -3,8 +3,8 @@
 // softmax over [prefix, own] is joined from parts: each part of the keys leaves its maximum, its sum of weights and its weighted sum of Values, and the parts are
 // brought to the greatest maximum.  The parts of a prefix take the columns of all the group's new tokens as one sequence's, with the keys that all of them see,
 // so a page is read once for 128 columns (32 in the kernel of few); what a sequence has behind the prefix is read as in gear_page_attn.  Both kinds of block run in one launch.
-// Bound by the matrix cores and exponentials of the prefix's tiles (questions about 6100 tokens, 2596 columns per KV head: 83 us, matrix cores 0.43 busy), by the bytes of what lies behind (64 sequences
-// of 100 to 1000 tokens behind 8192, 188 MB: 50 us), or, where both are small, by a block's chain of loads and joins (16 samples behind 2077 tokens, 32 heads: 12.7 us); and by the records, 520 bytes per
+// Bound by the matrix cores and exponentials of the prefix's tiles (questions about 6100 tokens, 2596 columns per KV head: 84 us, matrix cores 0.42 busy), by the bytes of what lies behind (64 sequences
+// of 100 to 1000 tokens behind 8192, 188 MB: 50 us), or, where both are small, by a block's chain of loads and joins (16 samples behind 2077 tokens, 32 heads: 13.1 us); and by the records, 520 bytes per
 // row and part, which the joining reads back.
 // A prefix counts to the last whole 64 tokens that every new token of the group sees, so that no key of it is masked from anyone; what is left of it is read with
 // each sequence's own tokens.
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(256) void page_merge_shared_kernel(SharedCall c, in
   // (what rounds to one part is one)
   const SharedKind& kind = few ? c.own_few : c.own_many;
   const int behind = sp.kv - span.begin, first_own = c.prefix.n_split;
-  const bool divided = kind.n_split > 1 && behind >= 2 * kind.least - kind.least / 2;
+  const bool divided = kind.n_split > 1 && behind - kind.least >= kind.least - kind.least / 2;
   if (before == 0 && !divided) return;   // (their one part is their output)
   auto join = [&](RowRecords<ONCE>& r, int j, int end) {   // a row's parts 0 .. before - 1 and first_own .. end - 1
     auto written = [&](int i) { return i < before || (i >= first_own && i < end); };
