@@ -353,7 +353,8 @@ typedef enum gear_rope_scaling {
   GEAR_ROPE_BASE = 2,     /* base * scale^(rot_dim / (rot_dim - 2)) in place of base: the slowest pair is w / scale    */
   GEAR_ROPE_TURNS = 3     /* by the turns u = trained_len * w / (2 pi) a pair makes over the trained length: w / scale  */
                           /* up to `low` turns, w from `high` on, and w (k + (1 - k) / scale), k = (u - low) / (high - low) */
-                          /* between (the ramp of YaRN, whose f is 0.1 ln(scale) + 1)                                  */
+                          /* between (the ramp in the paper on YaRN, whose f is 0.1 ln(scale) + 1; models whose ramp goes by the number of the */
+                          /* pair, between rounded bounds, have other frequencies: any may be given to gear_rope)             */
 } gear_rope_scaling;
 
 /* Fills host freq [rot_dim / 2].  base and scale are above 0; trained_len, low and high (0 <= low < high) count for GEAR_ROPE_TURNS only. */
@@ -435,9 +436,10 @@ int gear_page_move(const gear_page_config* cfg, void* pool, size_t pool_bytes, i
  */
 typedef struct gear_page_groups {
   int32_t n_groups;             /* up to 2^20                                                          */
-  int32_t max_q;                /* no group has more rows of q (the rows of one that has may stay)     */
+  int32_t max_q;                /* no group has more rows of q (one that has may share nothing; its rows are right) */
   int32_t max_prefix;           /* about the longest prefix: what the work is divided by               */
-  int32_t always;               /* 0: prefixes are shared where that is estimated to be faster, else the call is gear_page_attn's; */
+  int32_t always;               /* 0: prefixes are shared where that is estimated to be faster, else the call is gear_page_attn's (rows of q beyond */
+                                /* n_groups * max_q are taken to be those of sequences in no group, of up to max_kv tokens);                       */
                                 /* 1: always (but where a workspace of 512 MB would not do)            */
   const int32_t* group_start;   /* device [n_groups + 1], ascending: group i has sequences group_start[i] .. */
   const int32_t* prefix_len;    /* device [n_groups]: the first tokens that are the same in all of them; they are read through the row
